@@ -33,6 +33,8 @@
  *                         (cfg.buffer_layout; windows of epoch length)
  *   gram_mlp_encode_gather, gram_mlp_backward   steps 1 and 4 with a two-layer
  *                         stand-in encoder (cfg.d_hidden > 0)
+ *   gram_layer_norm, gram_attention (each with _backward), gram_attention_step
+ *                         the filter's own layer between H and dL/dH
  *
  * Memory.  Every pointer marked DEVICE is memory of the current HIP device,
  * owned by the caller (the library never frees, reallocates or keeps it beyond
@@ -368,6 +370,147 @@ int gram_window_import(gram_ctx* ctx, const int32_t* ids, const int64_t* counts,
 int gram_unique_static(const int32_t* ids, int64_t m, int32_t vocab_n, int32_t pad_id, int32_t* uniq,
                        int32_t* inverse, int32_t* counts, int32_t* u_dev, int32_t* err_dev, void* stream);
 
+/* ---- The collaborative filter's layer ------------------------------------------
+ * What stands between the positions' representations H and their gradient dL/dH
+ * when the filter is self-attention over the history (the news model of the
+ * paper's appendix D): layer norm and multi-head attention, forward and backward,
+ * and the attention of one new item per history over a cache, for serving.  Like
+ * gram_unique_static these calls need no context: they allocate nothing, never
+ * synchronise, keep nothing between calls and can be captured in a HIP graph.
+ * Calls may overlap as long as their outputs and work buffers are their own; the
+ * backward pass reads what its own work buffer was given in the same call only.
+ * Errors are reported through the return value and gram_last_error(NULL) of the
+ * calling thread.  All device memory belongs to the current device.
+ *
+ * Padding.  `segments` (DEVICE int32, one entry per position, nullable: no
+ * padding, one segment) says which session a position belongs to; a negative
+ * entry is padding.  Padding takes no part in anything, whatever it holds (NaN
+ * included): its outputs and gradients are zero and it adds nothing to any sum.
+ * With ids in hand: segments[p] = ids[p] == pad_id ? -1 : 0.
+ *
+ * Sums, softmax statistics and norms are float32 or wider, in a fixed order:
+ * results are the same bits run to run. */
+
+/* Layer norm of rows:  y = (x - mean) / sqrt(var + eps) * weight + bias.
+ *   x        DEVICE [m,d] of x_dtype     y  DEVICE [m,d] of y_dtype (may be x if
+ *            the types are the same), rounded to nearest even when bf16
+ *   weight, bias  DEVICE [d] float32     segments  DEVICE [m], nullable
+ *   m >= 0   d in [1, GRAM_LAYER_NORM_MAX_WIDTH]   eps finite, >= 0
+ *   stats    DEVICE [m,2] float32, nullable  out: mean and 1 / sqrt(var + eps) of
+ *            each row (zeros at padding), for the backward pass
+ * Widths that are multiples of 8 (or 4) with 16-byte aligned operands move 16 (8)
+ * bytes per load; any other width or alignment is served element by element. */
+#define GRAM_LAYER_NORM_MAX_WIDTH 8192
+int gram_layer_norm(const void* x, int32_t x_dtype, const float* weight, const float* bias,
+                    const int32_t* segments, int64_t m, int32_t d, float eps, void* y, int32_t y_dtype,
+                    float* stats, void* stream);
+
+/* Backward of the layer norm, at the x, weight, stats and segments of the forward.
+ *   dy       DEVICE [m,d] of y_dtype   gradient of y
+ *   add      DEVICE [m,d] float32, nullable  added to dx (the gradient that comes
+ *            past the layer in a residual block; may be dx itself)
+ *   dx       DEVICE [m,d] float32  out: the dL/dH that gram_grad_accumulate takes
+ *            (zero at padding, where add is not taken either)
+ *   dweight, dbias  DEVICE [d] float32  out (overwritten)
+ *   work     DEVICE, gram_layer_norm_work_bytes(m, d) bytes, 4-byte aligned */
+int64_t gram_layer_norm_work_bytes(int64_t m, int32_t d);
+int gram_layer_norm_backward(const void* x, int32_t x_dtype, const float* weight, const float* stats,
+                             const void* dy, int32_t y_dtype, const int32_t* segments, const float* add,
+                             int64_t m, int32_t d, float* dx, float* dweight, float* dbias, void* work,
+                             void* stream);
+
+/* Attention over histories.  For query position i and key position j of one
+ * history, query head h and the key head that it shares:
+ *   z = scale q_i . k_j      c = cap tanh(z / cap), or z if cap is 0
+ *   s = c + table[h, bucket(i - j)]          (no bias if buckets is 0)
+ *   o_i = sum_j softmax_j(s_ij) v_j          over the visible j
+ * j is visible to i if segments[i] == segments[j] >= 0 and, with causal set,
+ * j <= i or j < prefix.  A query that sees nothing yields a zero row.
+ *
+ * Buckets of a distance n = i - j, S of them to a side: n < S/2 (rounded down, e)
+ * has bucket n; a larger n has the largest b < S with
+ *   (n / e)^(S - e) >= (max_distance / e)^(b - e),
+ * that is e + floor((S - e) ln(n / e) / ln(max_distance / e)), S - 1 at most.  One
+ * side: S = buckets, keys after the query count as distance 0.  two_sided: S =
+ * buckets / 2, keys after the query have bucket S + bucket(j - i).
+ * gram_distance_bucket (HOST only) returns the bucket of i - j = distance, or -1. */
+#define GRAM_ATTENTION_MAX_LENGTH 262144
+#define GRAM_ATTENTION_MAX_BUCKETS 64
+typedef struct gram_attention_config {
+    int32_t heads;         /* query heads, a multiple of kv_heads (1..65535)          */
+    int32_t kv_heads;      /* heads of keys and values; heads / kv_heads share each   */
+    int32_t head_dim;      /* 1..128                                                  */
+    int32_t dtype;         /* gram_dtype of q, k, v, o and of their gradients         */
+    float scale;           /* finite                                                  */
+    float cap;             /* 0: none                                                 */
+    int32_t causal;        /* 0 or 1                                                  */
+    int32_t buckets;       /* 0: no bias; at most GRAM_ATTENTION_MAX_BUCKETS          */
+    int32_t max_distance;  /* > S/2 (see above), at most 2^30                         */
+    int32_t two_sided;     /* 0 or 1; then buckets is even                            */
+} gram_attention_config;
+
+/* Rows of an operand: element e of head h at row p of history b is
+ * data[b * batch_stride + p * row_stride + h * head_stride + e] (strides in
+ * elements).  Packed projections and caches are passed as they lie.  Where all
+ * operands of a call have 16-byte aligned rows, loads move 16 bytes (bf16 rows
+ * aligned to 8 bytes: 8), else single elements. */
+typedef struct gram_rows {
+    void* data;
+    int64_t batch_stride, row_stride, head_stride;
+} gram_rows;
+
+int32_t gram_distance_bucket(const gram_attention_config* cfg, int32_t distance);
+
+/*   q, o     [batch, length, heads, head_dim]     k, v  [batch, length, kv_heads, head_dim]
+ *   length   <= GRAM_ATTENTION_MAX_LENGTH; batch * heads * ceil(length / 64) <= 2^23
+ *   segments DEVICE [batch, length], nullable
+ *   prefix   DEVICE [batch], nullable (needs causal): keys before prefix[b] are
+ *            visible from earlier positions too (values <= 0: none)
+ *   table    DEVICE [heads, buckets] float32 (NULL if buckets is 0)
+ *   lse      DEVICE [batch, heads, length] float32, nullable  out: log sum_j exp s_ij
+ *            for the backward pass (-inf for a query that sees nothing)
+ * A NaN or infinity at a position reaches the outputs of the queries that see it
+ * and no others. */
+int gram_attention(const gram_attention_config* cfg, int32_t batch, int32_t length, const gram_rows* q,
+                   const gram_rows* k, const gram_rows* v, const gram_rows* o, const int32_t* segments,
+                   const int32_t* prefix, const float* table, float* lse, void* stream);
+
+/* Backward of gram_attention, at its operands and outputs.
+ *   dout     gradient of o, laid out as q           dq, dk, dv  out (overwritten),
+ *            laid out as q, k, v; dk and dv are summed over the heads that share them
+ *   dtable   DEVICE [heads, buckets] float32, nullable  out (overwritten): gradient
+ *            of table, summed over the batch
+ *   work     DEVICE, gram_attention_backward_bytes(cfg, batch, length) bytes,
+ *            16-byte aligned
+ * With bf16 operands the weights and their gradients are rounded to bf16 as they
+ * enter the matrix cores; dtable is summed from the unrounded ones. */
+int64_t gram_attention_backward_bytes(const gram_attention_config* cfg, int32_t batch, int32_t length);
+int gram_attention_backward(const gram_attention_config* cfg, int32_t batch, int32_t length,
+                            const gram_rows* q, const gram_rows* k, const gram_rows* v, const gram_rows* o,
+                            const float* lse, const gram_rows* dout, const gram_rows* dq, const gram_rows* dk,
+                            const gram_rows* dv, const int32_t* segments, const int32_t* prefix,
+                            const float* table, float* dtable, void* work, void* stream);
+
+/* Serving: one new item per history.  The new key and value are written to row
+ * lengths[b] of history b's cache and the new query, at that position, attends to
+ * rows first[b] .. lengths[b].
+ *   q, o     [batch, 1, heads, head_dim] (row_stride unused)
+ *   k_new, v_new      [batch, 1, kv_heads, head_dim] (row_stride unused)
+ *   k_cache, v_cache  [batch, capacity, kv_heads, head_dim]
+ *   lengths  DEVICE [batch]  items that the cache holds; outside [0, capacity) the
+ *            history is idle: its o is zero and its cache is left as it is.  The
+ *            caller advances lengths after the last layer
+ *   first    DEVICE [batch], nullable  first visible row (the start of the current
+ *            session, or of a window), clipped to [0, lengths[b]]
+ *   work     DEVICE, gram_attention_step_bytes(cfg, batch, capacity) bytes, 16-byte
+ *            aligned
+ * cfg's causal flag has no bearing here.  Rows that are not visible are not read. */
+int64_t gram_attention_step_bytes(const gram_attention_config* cfg, int32_t batch, int32_t capacity);
+int gram_attention_step(const gram_attention_config* cfg, int32_t batch, int32_t capacity, const gram_rows* q,
+                        const gram_rows* k_new, const gram_rows* v_new, const gram_rows* k_cache,
+                        const gram_rows* v_cache, const int32_t* lengths, const int32_t* first,
+                        const float* table, const gram_rows* o, void* work, void* stream);
+
 /* Synchronise `stream` and return (and clear) any latched device error. */
 int gram_check(gram_ctx* ctx, void* stream);
 
@@ -393,8 +536,8 @@ int gram_light_max(void);
 int gram_profile_enable(gram_ctx* ctx, uint64_t mask, int32_t max_launches);
 int gram_profile_read(gram_ctx* ctx, int k, int64_t* launches, double* total_ms);
 
-/* Message of the last failing call on ctx (or of the last failing gram_create
- * when ctx is NULL).  The string is owned by the library. */
+/* Message of the last failing call on ctx (or, when ctx is NULL, of the calling
+ * thread's last failing gram_create or call without a context).  The string is owned by the library. */
 const char* gram_last_error(const gram_ctx* ctx);
 
 #ifdef __cplusplus

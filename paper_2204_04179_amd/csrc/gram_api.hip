@@ -2,6 +2,7 @@
 // workspace layout, kernel sequencing.  No arithmetic of the method lives here.
 #include <stdarg.h>
 #include <stdio.h>
+#include <string.h>
 
 #include <mutex>
 #include <new>
@@ -12,7 +13,8 @@ using namespace gram;
 
 namespace {
 
-std::string g_create_error;
+// Message of the last failing call without a context; each thread has its own, since such calls may run side by side.
+thread_local char g_call_error[512] = "";
 
 int fail(Ctx* c, int code, const char* fmt, ...)
 {
@@ -21,7 +23,7 @@ int fail(Ctx* c, int code, const char* fmt, ...)
     va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    if (c) c->last_error = buf; else g_create_error = buf;
+    if (c) c->last_error = buf; else memcpy(g_call_error, buf, sizeof buf);
     return code;
 }
 
@@ -255,6 +257,19 @@ __global__ void k_copy_scalar(const int* __restrict__ src, int* __restrict__ dst
 }
 
 }  // namespace
+
+namespace gram {
+
+int fail_call(int code, const char* fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_call_error, sizeof g_call_error, fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+}  // namespace gram
 
 extern "C" {
 
@@ -796,7 +811,7 @@ int gram_check(gram_ctx* ctx, void* stream)
 const char* gram_last_error(const gram_ctx* ctx)
 {
     const Ctx* c = reinterpret_cast<const Ctx*>(ctx);
-    return c ? c->last_error.c_str() : g_create_error.c_str();
+    return c ? c->last_error.c_str() : g_call_error;
 }
 
 }  // extern "C"

@@ -357,6 +357,9 @@ bool encoder_wgrad(Ctx* c, const void* X, float* dW, hipStream_t s, int64_t firs
                    bool accumulate, const WgradRows* other = nullptr, float* export_G = nullptr,
                    const int* rank_of_slot = nullptr, const WindowMeta* meta = nullptr,
                    const LossSum* loss = nullptr);      // loss: also sum these (in the reduction's launch, if there is one)
+// Records the message of a failing call that has no context, for gram_last_error(NULL) on the calling thread; returns code.
+int fail_call(int code, const char* fmt, ...);
+
 // ---- gram_mlp.hip --------------------------------------------------------
 // Forward of the two-layer encoder for the unique items of the batch; A1 (nullable) receives the
 // bf16 hidden activations.  Return value as encode_forward.

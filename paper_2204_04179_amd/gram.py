@@ -24,6 +24,9 @@ EXPORTS = ("gram_workspace_bytes", "gram_create", "gram_destroy", "gram_unique",
            "gram_encoder_wgrad_chunk", "gram_pseudo_loss_grad", "gram_flush",
            "gram_flush64", "gram_window_end", "gram_window_import", "gram_mlp_encode_gather", "gram_mlp_batch_bytes",
            "gram_mlp_backward", "gram_unique_static",
+           "gram_layer_norm", "gram_layer_norm_backward", "gram_layer_norm_work_bytes", "gram_distance_bucket",
+           "gram_attention", "gram_attention_backward", "gram_attention_backward_bytes", "gram_attention_step",
+           "gram_attention_step_bytes",
            "gram_check", "gram_last_error",
            "gram_kernel_count", "gram_kernel_name", "gram_light_max", "gram_profile_enable",
            "gram_profile_read")
@@ -34,6 +37,17 @@ class GramConfig(C.Structure):
                 ("max_positions", C.c_int64), ("k_steps", C.c_int32), ("pad_id", C.c_int32),
                 ("u_total_cap", C.c_int64), ("xw_dtype", C.c_int32), ("buffer_layout", C.c_int32),
                 ("d_hidden", C.c_int32), ("h_dtype", C.c_int32)]
+
+
+class GramAttentionConfig(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("scale", C.c_float), ("cap", C.c_float), ("causal", C.c_int32), ("buckets", C.c_int32),
+                ("max_distance", C.c_int32), ("two_sided", C.c_int32)]
+
+
+class GramRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("row_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
 
 
 class GramError(RuntimeError):
@@ -96,6 +110,26 @@ def load():
     L.gram_window_import.argtypes = [vp, vp, vp, vp, C.c_int64, vp]
     L.gram_unique_static.restype = C.c_int
     L.gram_unique_static.argtypes = [vp, C.c_int64, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp]
+    i32, i64, f32 = C.c_int32, C.c_int64, C.c_float
+    acp, rp = C.POINTER(GramAttentionConfig), C.POINTER(GramRows)
+    L.gram_layer_norm.restype = C.c_int
+    L.gram_layer_norm.argtypes = [vp, i32, vp, vp, vp, i64, i32, f32, vp, i32, vp, vp]
+    L.gram_layer_norm_work_bytes.restype = i64
+    L.gram_layer_norm_work_bytes.argtypes = [i64, i32]
+    L.gram_layer_norm_backward.restype = C.c_int
+    L.gram_layer_norm_backward.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp, i64, i32, vp, vp, vp, vp, vp]
+    L.gram_distance_bucket.restype = i32
+    L.gram_distance_bucket.argtypes = [acp, i32]
+    L.gram_attention.restype = C.c_int
+    L.gram_attention.argtypes = [acp, i32, i32, rp, rp, rp, rp, vp, vp, vp, vp, vp]
+    L.gram_attention_backward_bytes.restype = i64
+    L.gram_attention_backward_bytes.argtypes = [acp, i32, i32]
+    L.gram_attention_backward.restype = C.c_int
+    L.gram_attention_backward.argtypes = [acp, i32, i32, rp, rp, rp, rp, vp, rp, rp, rp, rp, vp, vp, vp, vp, vp, vp]
+    L.gram_attention_step_bytes.restype = i64
+    L.gram_attention_step_bytes.argtypes = [acp, i32, i32]
+    L.gram_attention_step.restype = C.c_int
+    L.gram_attention_step.argtypes = [acp, i32, i32, rp, rp, rp, rp, rp, vp, vp, vp, rp, vp, vp]
     L.gram_check.restype = C.c_int
     L.gram_check.argtypes = [vp, vp]
     L.gram_last_error.restype = C.c_char_p
@@ -168,6 +202,201 @@ def unique_static(ids, vocab_n, pad_id, uniq, inverse, counts, u_dev, err_dev=No
                               _stream(stream))
     if rc != OK:
         raise GramError(rc, (L.gram_last_error(None) or b"").decode())
+
+
+# ---- the collaborative filter's layer: calls without a context --------------------------------------------
+
+
+def _ck_call(rc):
+    if rc != OK:
+        raise GramError(rc, (load().gram_last_error(None) or b"").decode())
+
+
+def _refuse(message):
+    raise GramError(ERR_ARG, message)
+
+
+def _dtype_of(t, what):
+    import torch
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    _refuse(f"{what}: float32 or bfloat16 expected, got {t.dtype}")
+
+
+def _flat(t, what, dtype, numel):
+    """Pointer of a contiguous tensor of that type and number of elements on the current device (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
+        _refuse(f"{what}: a contiguous {dtype} tensor of {numel} elements expected, got {t.dtype} {tuple(t.shape)}")
+    _here(t, what)
+    return t.data_ptr()
+
+
+def _here(t, what):
+    import torch
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        _refuse(f"{what}: not on the current device")
+
+
+def _bytes_of(work, what, size):
+    if work is None or work.numel() * work.element_size() < size or not work.is_contiguous():
+        _refuse(f"{what}: a contiguous work buffer of at least {size} bytes expected")
+    _here(work, what)
+    return work.data_ptr()
+
+
+def layer_norm_work_bytes(m, d):
+    return int(load().gram_layer_norm_work_bytes(int(m), int(d)))
+
+
+def _norm_rows(x, what):
+    if x.dim() < 1 or not x.is_contiguous():
+        _refuse(f"{what}: contiguous rows expected")
+    d = x.shape[-1]
+    return (x.numel() // d if d else 0), d
+
+
+def layer_norm(x, weight, bias, y, stats=None, segments=None, eps=1e-5, stream=None):
+    """gram_layer_norm: y = (x - mean) * rstd * weight + bias over the last dimension of x.  x and y are float32 or
+    bfloat16, independently; stats ([rows, 2], float32) keeps mean and rstd for the backward pass; rows whose segment is
+    negative are padding and become zero."""
+    import torch
+    m, d = _norm_rows(x, "layer_norm: x")
+    f32 = torch.float32
+    if y.shape != x.shape or not y.is_contiguous():
+        _refuse("layer_norm: y must be contiguous, of x's shape")
+    _here(x, "layer_norm: x"), _here(y, "layer_norm: y")
+    _ck_call(load().gram_layer_norm(x.data_ptr(), _dtype_of(x, "layer_norm: x"), _flat(weight, "layer_norm: weight", f32, d),
+                                    _flat(bias, "layer_norm: bias", f32, d),
+                                    _flat(segments, "layer_norm: segments", torch.int32, m), m, d, eps, y.data_ptr(),
+                                    _dtype_of(y, "layer_norm: y"), _flat(stats, "layer_norm: stats", f32, 2 * m),
+                                    _stream(stream)))
+
+
+def layer_norm_backward(x, weight, stats, dy, dx, dweight, dbias, work, segments=None, add=None, stream=None):
+    """gram_layer_norm_backward: dx (float32, plus `add` where given), dweight and dbias of layer_norm; work:
+    layer_norm_work_bytes(rows, d) bytes."""
+    import torch
+    what = "layer_norm_backward: "
+    m, d = _norm_rows(x, what + "x")
+    f32 = torch.float32
+    if dy.shape != x.shape or not dy.is_contiguous():
+        _refuse(what + "dy must be contiguous, of x's shape")
+    _here(x, what + "x"), _here(dy, what + "dy")
+    L = load()
+    _ck_call(L.gram_layer_norm_backward(x.data_ptr(), _dtype_of(x, what + "x"), _flat(weight, what + "weight", f32, d),
+                                        _flat(stats, what + "stats", f32, 2 * m), dy.data_ptr(), _dtype_of(dy, what + "dy"),
+                                        _flat(segments, what + "segments", torch.int32, m),
+                                        _flat(add, what + "add", f32, m * d), m, d, _flat(dx, what + "dx", f32, m * d),
+                                        _flat(dweight, what + "dweight", f32, d), _flat(dbias, what + "dbias", f32, d),
+                                        _bytes_of(work, what + "work", L.gram_layer_norm_work_bytes(m, d)), _stream(stream)))
+
+
+class HistoryAttention:
+    """Multi-head attention over item histories (gram_attention and its backward, gram_attention_step): the settings of
+    a layer, which holds no device memory and may be used by any number of calls at once.
+
+    q, o and their gradients are [batch, length, heads, head_dim] tensors, k and v [batch, length, kv_heads, head_dim],
+    with any strides but a contiguous last dimension (views of a packed projection, a cache)."""
+
+    def __init__(self, heads, kv_heads, head_dim, dtype=BF16, scale=None, cap=0.0, causal=True, buckets=0, max_distance=0,
+                 two_sided=False):
+        import torch
+        self._lib = load()
+        self.heads, self.kv_heads, self.head_dim, self.buckets = int(heads), int(kv_heads), int(head_dim), int(buckets)
+        self.dtype = torch.bfloat16 if dtype == BF16 else torch.float32
+        self.cfg = GramAttentionConfig(self.heads, self.kv_heads, self.head_dim, int(dtype),
+                                       float(head_dim) ** -0.5 if scale is None else float(scale), float(cap),
+                                       1 if causal else 0, self.buckets, int(max_distance), 1 if two_sided else 0)
+        self._cfg = C.byref(self.cfg)
+        _ck_call(self._lib.gram_attention(self._cfg, 0, 0, None, None, None, None, None, None, None, None, None))
+
+    def bucket(self, distance):
+        """The bucket of the distance query position minus key position (-1 without a bias)."""
+        return int(self._lib.gram_distance_bucket(self._cfg, int(distance)))
+
+    def _rows(self, t, what, batch, rows, heads):
+        st = t.stride()
+        if tuple(t.shape) != (batch, rows, heads, self.head_dim) or t.dtype is not self.dtype or \
+                (st[3] != 1 and self.head_dim != 1):
+            _refuse(f"{what}: {self.dtype} [{batch}, {rows}, {heads}, {self.head_dim}] with a contiguous last dimension "
+                    f"expected, got {t.dtype} {tuple(t.shape)}")
+        _here(t, what)
+        return C.byref(GramRows(t.data_ptr(), st[0], st[1], st[2]))
+
+    def _row(self, t, what, batch, heads):
+        st = t.stride()
+        if tuple(t.shape) != (batch, heads, self.head_dim) or t.dtype is not self.dtype or (st[2] != 1 and self.head_dim != 1):
+            _refuse(f"{what}: {self.dtype} [{batch}, {heads}, {self.head_dim}] with a contiguous last dimension expected, "
+                    f"got {t.dtype} {tuple(t.shape)}")
+        _here(t, what)
+        return C.byref(GramRows(t.data_ptr(), st[0], 0, st[1]))
+
+    def _table(self, t, what):
+        import torch
+        if (t is None) != (self.buckets == 0):
+            _refuse(f"{what}: given exactly when the layer has buckets")
+        return _flat(t, what, torch.float32, self.heads * self.buckets)
+
+    def _sizes(self, q, what):
+        if q.dim() != 4:
+            _refuse(f"{what}: [batch, length, heads, head_dim] expected")
+        return q.shape[0], q.shape[1]
+
+    def forward(self, q, k, v, o, lse=None, segments=None, prefix=None, table=None, stream=None):
+        """o = attention of q over k, v.  lse ([batch, heads, length], float32) is kept for the backward pass; segments
+        (int32 [batch, length], negative: padding) and prefix (int32 [batch]) mask; table ([heads, buckets], float32)."""
+        import torch
+        B, L = self._sizes(q, "forward: q")
+        H, KV = self.heads, self.kv_heads
+        _ck_call(self._lib.gram_attention(
+            self._cfg, B, L, self._rows(q, "forward: q", B, L, H), self._rows(k, "forward: k", B, L, KV),
+            self._rows(v, "forward: v", B, L, KV), self._rows(o, "forward: o", B, L, H),
+            _flat(segments, "forward: segments", torch.int32, B * L), _flat(prefix, "forward: prefix", torch.int32, B),
+            self._table(table, "forward: table"), _flat(lse, "forward: lse", torch.float32, B * H * L), _stream(stream)))
+
+    def backward_bytes(self, batch, length):
+        return int(self._lib.gram_attention_backward_bytes(self._cfg, int(batch), int(length)))
+
+    def backward(self, q, k, v, o, lse, do, dq, dk, dv, work, segments=None, prefix=None, table=None, dtable=None,
+                 stream=None):
+        """dq, dk, dv and, where given, dtable from the gradient `do` of o, at the operands and outputs of forward; work:
+        backward_bytes(batch, length) bytes."""
+        import torch
+        B, L = self._sizes(q, "backward: q")
+        H, KV, i32, f32 = self.heads, self.kv_heads, torch.int32, torch.float32
+        rows = self._rows
+        if dtable is not None and self.buckets == 0:
+            _refuse("backward: dtable without buckets")
+        _ck_call(self._lib.gram_attention_backward(
+            self._cfg, B, L, rows(q, "backward: q", B, L, H), rows(k, "backward: k", B, L, KV),
+            rows(v, "backward: v", B, L, KV), rows(o, "backward: o", B, L, H), _flat(lse, "backward: lse", f32, B * H * L),
+            rows(do, "backward: do", B, L, H), rows(dq, "backward: dq", B, L, H), rows(dk, "backward: dk", B, L, KV),
+            rows(dv, "backward: dv", B, L, KV), _flat(segments, "backward: segments", i32, B * L),
+            _flat(prefix, "backward: prefix", i32, B), self._table(table, "backward: table"),
+            _flat(dtable, "backward: dtable", f32, H * self.buckets),
+            _bytes_of(work, "backward: work", self._lib.gram_attention_backward_bytes(self._cfg, B, L)), _stream(stream)))
+
+    def step_bytes(self, batch, capacity):
+        return int(self._lib.gram_attention_step_bytes(self._cfg, int(batch), int(capacity)))
+
+    def step(self, q, k_new, v_new, k_cache, v_cache, lengths, o, work, first=None, table=None, stream=None):
+        """One new item per history: k_new, v_new ([batch, kv_heads, head_dim]) are written to row lengths[b] of the
+        caches ([batch, capacity, kv_heads, head_dim]) and q ([batch, heads, head_dim]) attends to rows first[b] to
+        lengths[b]; work: step_bytes(batch, capacity) bytes."""
+        import torch
+        if q.dim() != 3 or k_cache.dim() != 4:
+            _refuse("step: q [batch, heads, head_dim] and caches [batch, capacity, kv_heads, head_dim] expected")
+        B, cap, H, KV, i32 = q.shape[0], k_cache.shape[1], self.heads, self.kv_heads, torch.int32
+        _ck_call(self._lib.gram_attention_step(
+            self._cfg, B, cap, self._row(q, "step: q", B, H), self._row(k_new, "step: k_new", B, KV),
+            self._row(v_new, "step: v_new", B, KV), self._rows(k_cache, "step: k_cache", B, cap, KV),
+            self._rows(v_cache, "step: v_cache", B, cap, KV), _flat(lengths, "step: lengths", i32, B),
+            _flat(first, "step: first", i32, B), self._table(table, "step: table"), self._row(o, "step: o", B, H),
+            _bytes_of(work, "step: work", self._lib.gram_attention_step_bytes(self._cfg, B, cap)), _stream(stream)))
 
 
 class Gram:

@@ -1,0 +1,204 @@
+"""Layer norm, attention over histories and its cached step on the GPU, against their definitions in 64 bits with bounds
+that count roundings (tests/layer_oracle.py)."""
+import pytest
+
+import layer_oracle as lo
+
+pytestmark = pytest.mark.gpu
+
+
+def draw(torch, shape, seed, dtype, scale=1.0, mean=0.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale + mean).to(dtype)
+
+
+# ---- layer norm -------------------------------------------------------------------------------------------
+
+NORMS = [
+    # rows, width, x, y, padding
+    (1, 1, "f32", "f32", False), (1, 8, "bf16", "bf16", False), (3, 7, "f32", "bf16", True), (64, 32, "f32", "f32", False),
+    (17, 128, "bf16", "f32", True), (5, 129, "bf16", "bf16", False), (33, 400, "f32", "bf16", True),
+    (130, 256, "bf16", "bf16", True), (19, 260, "f32", "f32", False), (9, 512, "f32", "f32", True),
+    (7, 516, "bf16", "bf16", False), (65, 1024, "bf16", "bf16", False), (4, 1028, "f32", "bf16", False),
+    (2, 1500, "f32", "f32", True), (3, 2048, "bf16", "f32", False), (3, 2056, "bf16", "bf16", True),
+    (2, 8192, "f32", "f32", False), (2, 8191, "bf16", "bf16", False), (2, 5004, "f32", "bf16", False),
+    (40_003, 24, "bf16", "bf16", True), (20_000, 96, "f32", "f32", False),
+]
+
+
+@pytest.mark.parametrize("M,d,xt,yt,padded", NORMS)
+def test_layer_norm_and_its_backward(M, d, xt, yt, padded):
+    import torch
+    from paper_2204_04179_amd import gram
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}
+    x, w, b = draw(torch, (M, d), 1, t[xt], 1.5, 0.7), draw(torch, (d,), 2, torch.float32, 0.3, 1.0), draw(torch, (d,), 3, torch.float32)
+    dy, add = draw(torch, (M, d), 4, t[yt]), draw(torch, (M, d), 5, torch.float32)
+    seg = None
+    if padded:
+        seg = (torch.arange(M) % 3 - 1).to(torch.int32)
+        x[seg < 0], dy[seg < 0], add[seg < 0] = float("nan"), float("inf"), float("nan")
+    ref = lo.layer_norm(x, w, b, t[yt], seg, dy=dy, add=add)
+    X, W, Bi, DY, A = (v.cuda() for v in (x, w, b, dy, add))
+    S = None if seg is None else seg.cuda()
+    y = torch.full((M, d), float("nan"), dtype=t[yt], device="cuda")
+    stats = torch.full((M, 2), float("nan"), device="cuda")
+    gram.layer_norm(X, W, Bi, y, stats=stats, segments=S)
+    dx, dw, db = (torch.full(s, float("nan"), device="cuda") for s in ((M, d), (d,), (d,)))
+    work = torch.empty(gram.layer_norm_work_bytes(M, d), dtype=torch.uint8, device="cuda")
+    gram.layer_norm_backward(X, W, stats, DY, dx, dw, db, work, segments=S, add=A)
+    for n, got in (("y", y), ("dx", dx), ("dw", dw), ("db", db)):
+        lo.assert_within(got, ref[n], n)
+    plain = torch.empty_like(dx)
+    gram.layer_norm_backward(X, W, stats, DY, plain, dw, db, work, segments=S)
+    lo.assert_within(plain, lo.layer_norm(x, w, b, t[yt], seg, dy=dy)["dx"], "dx without add")
+
+
+# ---- attention --------------------------------------------------------------------------------------------
+
+
+def case(dtype, B, L, H, KV, D, causal=True, prefix=False, docs=False, pad=None, cap=0.0, buckets=0, far=0, both=False,
+         layout="packed"):
+    return dict(dtype=dtype, B=B, L=L, H=H, KV=KV, D=D, causal=causal, prefix=prefix, docs=docs, pad=pad, cap=cap,
+                buckets=buckets, far=far, both=both, layout=layout)
+
+
+CASES = [
+    case("f32", 1, 1, 1, 1, 1), case("bf16", 1, 1, 1, 1, 8, buckets=2, far=3), case("bf16", 3, 2, 2, 1, 16, causal=False),
+    case("f32", 2, 3, 3, 1, 5, buckets=1, far=2), case("bf16", 2, 15, 4, 2, 20, pad="tail", buckets=32, far=64),
+    case("f32", 4, 16, 2, 2, 16, pad="tail"), case("bf16", 2, 16, 1, 1, 33, causal=False, buckets=8, far=9, both=True),
+    case("bf16", 3, 55, 4, 4, 20, prefix=True, buckets=32, far=64, both=True), case("bf16", 2, 63, 5, 1, 32, cap=5.0),
+    case("f32", 2, 64, 2, 2, 64, buckets=32, far=128), case("bf16", 2, 64, 2, 2, 64, buckets=32, far=128),
+    case("bf16", 2, 65, 2, 2, 128, pad="all", buckets=16, far=40), case("f32", 2, 65, 2, 1, 128, pad="holes", cap=3.0),
+    case("bf16", 2, 100, 4, 4, 64, pad="tail", buckets=32, far=128), case("f32", 1, 100, 4, 2, 100, docs=True, buckets=12, far=40),
+    case("bf16", 2, 127, 2, 2, 40, docs=True, pad="holes", layout="heads"), case("bf16", 1, 128, 2, 1, 96, causal=False),
+    case("f32", 1, 129, 3, 3, 24, causal=False, docs=True, cap=20.0, buckets=32, far=256, both=True),
+    case("bf16", 2, 200, 2, 2, 128, buckets=32, far=128), case("bf16", 1, 200, 8, 2, 64, prefix=True, pad="tail", cap=30.0),
+    case("f32", 1, 257, 2, 2, 32, prefix=True, docs=True, buckets=64, far=100, both=True),
+    case("bf16", 1, 300, 10, 2, 36, causal=False, pad="holes", buckets=64, far=512, both=True, layout="heads"),
+    case("bf16", 1, 515, 2, 1, 127, docs=True, cap=10.0, buckets=16, far=64, layout="odd"),
+    case("f32", 1, 515, 1, 1, 63, layout="odd"), case("bf16", 1, 1003, 2, 1, 64, docs=True, pad="tail", buckets=32, far=128),
+]
+
+
+def inputs(torch, c, seed=0):
+    B, L, H, KV, D = c["B"], c["L"], c["H"], c["KV"], c["D"]
+    dt = torch.float32 if c["dtype"] == "f32" else torch.bfloat16
+    q, k, v, do = (draw(torch, (B, L, n, D), seed + i, dt) for i, n in enumerate((H, KV, KV, H)))
+    seg = None
+    if c["docs"]:
+        g = torch.Generator().manual_seed(seed + 50)
+        seg = torch.cumsum((torch.rand(B, L, generator=g) < 3.0 / L).int(), 1).int()
+    if c["pad"]:
+        seg = torch.zeros(B, L, dtype=torch.int32) if seg is None else seg
+        if c["pad"] == "tail":
+            seg[0, L - min(3, L - 1):] = -1
+            seg[-1, L // 3 + 1:] = -1
+        elif c["pad"] == "holes":
+            seg[:, ::7] = -5
+        else:
+            seg[0] = -1                                     # a history of padding only
+    prefix = torch.arange(B, dtype=torch.int32) * 17 + L // 2 if c["prefix"] else None
+    table = draw(torch, (H, c["buckets"]), seed + 9, torch.float32) if c["buckets"] else None
+    return q, k, v, do, seg, prefix, table
+
+
+def placed(torch, t, layout):
+    """t on the GPU behind the strides that `layout` stands for."""
+    B, L, n, D = t.shape
+    if layout == "packed":                                  # heads in the middle of wider rows
+        box = torch.full((B, L, n + 3, D), float("nan"), dtype=t.dtype, device="cuda")
+        out = box[:, :, 2:2 + n]
+    elif layout == "heads":                                 # [B, heads, L, D]
+        out = torch.full((B, n, L, D), float("nan"), dtype=t.dtype, device="cuda").transpose(1, 2)
+    else:                                                   # rows of no aligned length, off by one element
+        box = torch.full((B * L * (n * D + 1) + 1,), float("nan"), dtype=t.dtype, device="cuda")
+        out = torch.as_strided(box, (B, L, n, D), (L * (n * D + 1), n * D + 1, D, 1), 1)
+    out.copy_(t)
+    return out
+
+
+def plan_of(gram, c):
+    return gram.HistoryAttention(c["H"], c["KV"], c["D"], dtype=gram.F32 if c["dtype"] == "f32" else gram.BF16, cap=c["cap"],
+                                 causal=c["causal"], buckets=c["buckets"], max_distance=c["far"], two_sided=c["both"])
+
+
+def oracle_of(c, q, k, v, do, seg, prefix, table):
+    return lo.attention(q, k, v, scale=c["D"] ** -0.5, cap=c["cap"], causal=c["causal"], segments=seg, prefix=prefix, table=table,
+                        far=c["far"], both=c["both"], do=do)
+
+
+def run_gpu(torch, gram, c, q, k, v, do, seg, prefix, table, backward=True):
+    plan = plan_of(gram, c)
+    B, L, H = c["B"], c["L"], c["H"]
+    Q, K, V, DO = (placed(torch, t, c["layout"]) for t in (q, k, v, do))
+    O, DQ, DK, DV = (placed(torch, torch.full_like(t, float("nan")), c["layout"]) for t in (q, q, k, v))
+    seg, prefix, table = (None if t is None else t.cuda() for t in (seg, prefix, table))
+    lse = torch.full((B, H, L), float("nan"), device="cuda")
+    plan.forward(Q, K, V, O, lse=lse, segments=seg, prefix=prefix, table=table)
+    out = dict(o=O, lse=lse)
+    if backward:
+        work = torch.empty(plan.backward_bytes(B, L), dtype=torch.uint8, device="cuda")
+        dtable = torch.full((H, c["buckets"]), float("nan"), device="cuda") if c["buckets"] else None
+        plan.backward(Q, K, V, O, lse, DO, DQ, DK, DV, work, segments=seg, prefix=prefix, table=table, dtable=dtable)
+        out.update(dq=DQ, dk=DK, dv=DV)
+        if dtable is not None:
+            out["dtable"] = dtable
+    return out
+
+
+def name_of(c):
+    return "-".join(f"{k}{v}" for k, v in c.items() if v not in (False, None, 0, 0.0))
+
+
+@pytest.mark.parametrize("c", CASES, ids=name_of)
+def test_attention_and_its_backward(c):
+    import torch
+    from paper_2204_04179_amd import gram
+    data = inputs(torch, c)
+    want = oracle_of(c, *data)
+    got = run_gpu(torch, gram, c, *data)
+    for n in got:
+        lo.assert_within(got[n], want[n], n)
+
+
+# ---- one cached step --------------------------------------------------------------------------------------
+
+STEPS = [
+    # dtype, histories, capacity, heads, key heads, width, cap, buckets, far, both, first, layout
+    ("f32", 1, 1, 1, 1, 1, 0.0, 0, 0, False, False, "rows"), ("bf16", 3, 7, 2, 2, 8, 0.0, 2, 3, False, False, "rows"),
+    ("bf16", 4, 64, 4, 4, 64, 0.0, 32, 128, False, False, "rows"), ("f32", 5, 65, 5, 1, 20, 2.0, 8, 20, True, True, "rows"),
+    ("bf16", 6, 200, 8, 2, 128, 30.0, 32, 128, False, False, "heads"), ("bf16", 2, 513, 9, 1, 36, 0.0, 12, 40, False, True, "rows"),
+    ("f32", 2, 1024, 6, 2, 128, 0.0, 0, 0, False, False, "heads"), ("bf16", 3, 1500, 4, 1, 33, 5.0, 64, 700, False, False, "odd"),
+    ("bf16", 2, 3000, 16, 2, 96, 0.0, 16, 64, False, True, "rows"),
+]
+
+
+@pytest.mark.parametrize("dtype,B,cap_rows,H,KV,D,cap,buckets,far,both,first,layout", STEPS)
+def test_cached_step(dtype, B, cap_rows, H, KV, D, cap, buckets, far, both, first, layout):
+    import torch
+    from paper_2204_04179_amd import gram
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    q, kn, vn = draw(torch, (B, H, D), 1, dt), draw(torch, (B, KV, D), 2, dt), draw(torch, (B, KV, D), 3, dt)
+    kc, vc = draw(torch, (B, cap_rows, KV, D), 4, dt), draw(torch, (B, cap_rows, KV, D), 5, dt)
+    lens = torch.tensor([(cap_rows - 1, -1, cap_rows, 0, cap_rows // 2, cap_rows // 3)[b % 6] for b in range(B)], dtype=torch.int32)
+    for b in range(B):                                     # rows that the cache does not hold yet
+        if 0 <= lens[b] < cap_rows:
+            kc[b, lens[b]:], vc[b, lens[b]:] = float("nan"), float("inf")
+    start = (lens // 2 - 1 + torch.arange(B, dtype=torch.int32)) if first else None
+    if first:
+        for b in range(B):
+            if 0 <= lens[b] < cap_rows:
+                s = min(max(int(start[b]), 0), int(lens[b]))
+                kc[b, :s], vc[b, :s] = float("inf"), float("nan")
+    table = draw(torch, (H, buckets), 6, torch.float32) if buckets else None
+    o, bound, kw, vw = lo.step(q, kn, vn, kc, vc, lens, scale=D ** -0.5, cap=cap, first=start, table=table, far=far, both=both)
+    plan = gram.HistoryAttention(H, KV, D, dtype=gram.F32 if dtype == "f32" else gram.BF16, cap=cap, buckets=buckets,
+                                 max_distance=far, two_sided=both)
+    KC, VC = placed(torch, kc, "packed" if layout == "rows" else layout), placed(torch, vc, "packed" if layout == "rows" else layout)
+    O = torch.full((B, H, D), float("nan"), dtype=dt, device="cuda")
+    work = torch.empty(plan.step_bytes(B, cap_rows), dtype=torch.uint8, device="cuda")
+    plan.step(q.cuda(), kn.cuda(), vn.cuda(), KC, VC, lens.cuda(), O, work, first=None if start is None else start.cuda(),
+              table=None if table is None else table.cuda())
+    lo.assert_within(O, (o, bound), "o")
+    for got, want, what in ((KC, kw, "k_cache"), (VC, vw, "v_cache")):
+        assert torch.equal(torch.nan_to_num(got.cpu().float(), 7.0, 8.0, 9.0), torch.nan_to_num(want.float(), 7.0, 8.0, 9.0)), what
