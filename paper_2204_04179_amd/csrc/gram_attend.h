@@ -43,6 +43,8 @@ struct AttBuckets {
     int exact;
     int two_sided;
     int borders;             // side - 1 - exact of them, ascending
+    int last;                // from this distance on: bucket side - 1
+    float inv_exact, per_log2;      // the bucket is near exact + per_log2 log2(n inv_exact)
     int border[kMaxBorders];
 };
 
@@ -55,11 +57,18 @@ struct AttArgs {
     float* delta;            // [batch, heads, length]
     float* part;             // partial gradients of the table: [heads, parts, buckets]
     int batch, length, heads, kv_heads, group, dim;
-    int causal, unit;        // unit: bytes per global load and store of an operand row (16, 8, or one element)
+    int causal;
     int items, parts;
     float scale, cap;
     AttBuckets bk;
 };
+
+// The kernel's argument block where it lies in memory, to hand to a function that is called: the address of the parameter
+// itself would make every lane keep a copy of it.  For kernels whose one parameter is an AttArgs.
+__device__ __forceinline__ const AttArgs& kernel_args()
+{
+    return *(const AttArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+}
 
 // By value: a bit cast applied to an element of a vector yields the vector's first element.
 __device__ __forceinline__ float as_f32(uint32_t bits) { return __builtin_bit_cast(float, bits); }
@@ -82,38 +91,54 @@ template <int NCH> __device__ __forceinline__ int swz(int row)
 
 // ---- global rows ------------------------------------------------------------------------------------------
 
-// One 16-byte chunk of a row of `dim` elements, zeros behind them.  unit: what alignment allows per load.
-template <typename T> __device__ __forceinline__ u32x4 load_chunk(const T* __restrict__ row, int ch, int dim, int unit)
+// Rows [0, rows) of an operand, `stride` bytes apart, through a buffer descriptor: what lies behind the last of them
+// reads as zero.  The host keeps stride below 2^26, so that 64 rows stay within the descriptor's 32-bit offsets.
+constexpr uint32_t kAttBufferFlags = 0x00027000;     // 32-bit elements, no swizzle
+constexpr uint32_t kNowhere = 0xffffff00u;        // an offset behind every descriptor's end
+constexpr int64_t kAttMaxRowBytes = (int64_t)1 << 26;
+
+struct RowSource {
+    __amdgpu_buffer_rsrc_t rsrc;
+    uint32_t stride;
+};
+template <typename T> __device__ __forceinline__ RowSource row_source(const T* base, int64_t sr, int rows, int dim)
+{
+    const uint32_t stride = (uint32_t)sr * (uint32_t)sizeof(T);
+    const uint32_t bytes = rows > 0 ? (uint32_t)((rows < kTile ? rows : kTile) - 1) * stride + (uint32_t)dim * (uint32_t)sizeof(T) : 0u;
+    return {__builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, bytes, kAttBufferFlags), stride};
+}
+
+// The 16-byte chunk `ch` of a row that begins at byte `off`, zeros behind its `dim` elements.  UNIT: the bytes per load that
+// the alignment of all operands allows (16; 8 with bf16; one element).
+template <typename T, int UNIT> __device__ __forceinline__ u32x4 load_chunk(const RowSource& src, uint32_t off, int ch, int dim)
 {
     constexpr int EPC = 16 / sizeof(T);
     const int at = ch * EPC;
-    u32x4 v = {0u, 0u, 0u, 0u};
-    if (unit == 16) {
-        if (at < dim) v = *reinterpret_cast<const u32x4*>(row + at);
-    } else if (sizeof(T) == 2 && unit == 8) {
-        if (at < dim) {
-            const u32x2 t = *reinterpret_cast<const u32x2*>(row + at);
-            v[0] = t[0], v[1] = t[1];
-        }
-        if (at + 4 < dim) {
-            const u32x2 t = *reinterpret_cast<const u32x2*>(row + at + 4);
-            v[2] = t[0], v[3] = t[1];
-        }
+    const uint32_t byte = off + (uint32_t)ch * 16u;
+    if constexpr (UNIT == 16) {
+        return __builtin_amdgcn_raw_buffer_load_b128(src.rsrc, at < dim ? byte : kNowhere, 0, 0);
+    } else if constexpr (UNIT == 8) {
+        const u32x2 lo = __builtin_amdgcn_raw_buffer_load_b64(src.rsrc, at < dim ? byte : kNowhere, 0, 0);
+        const u32x2 hi = __builtin_amdgcn_raw_buffer_load_b64(src.rsrc, at + 4 < dim ? byte + 8u : kNowhere, 0, 0);
+        return u32x4{lo[0], lo[1], hi[0], hi[1]};
     } else {
+        u32x4 v = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int e = 0; e < EPC; ++e)
-            if (at + e < dim) {
-                if constexpr (sizeof(T) == 2) v[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[at + e] << (16 * (e & 1));
-                else v[e] = reinterpret_cast<const uint32_t*>(row)[at + e];
-            }
+        for (int e = 0; e < EPC; ++e) {
+            const uint32_t where = at + e < dim ? byte + (uint32_t)(e * sizeof(T)) : kNowhere;
+            if constexpr (sizeof(T) == 2)
+                v[e / 2] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(src.rsrc, where, 0, 0) << (16 * (e & 1));
+            else
+                v[e] = __builtin_amdgcn_raw_buffer_load_b32(src.rsrc, where, 0, 0);
+        }
+        return v;
     }
-    return v;
 }
 
 // Four neighbouring elements at column `at`.
-template <typename T> __device__ __forceinline__ void store4(T* __restrict__ row, int at, int dim, int unit, f32x4 v)
+template <typename T, int UNIT> __device__ __forceinline__ void store4(T* __restrict__ row, int at, int dim, f32x4 v)
 {
-    if (unit >= 8) {                 // rows are whole groups of four elements
+    if constexpr (UNIT >= 8) {       // rows are whole groups of four elements
         if (at < dim) {
             if constexpr (sizeof(T) == 2) {
                 const u32x2 t = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -133,6 +158,27 @@ template <typename T> __device__ __forceinline__ void store4(T* __restrict__ row
 }
 
 __device__ __forceinline__ bool nonfinite_bits(uint32_t f32_bits) { return (f32_bits & 0x7f800000u) == 0x7f800000u; }
+
+// Collects what has_nonfinite needs of a chunk: the largest exponent seen, for each 16-bit half (bf16) or word.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+template <typename T> __device__ __forceinline__ uint32_t max_exponent(uint32_t most, u32x4 v)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t x = v[e] & 0x7f807f80u;
+            most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most), __builtin_bit_cast(u16x2, x)));
+        } else {
+            const uint32_t x = v[e] & 0x7f800000u;
+            most = most > x ? most : x;
+        }
+    }
+    return most;
+}
+template <typename T> __device__ __forceinline__ bool has_nonfinite(uint32_t most)
+{
+    return (most & 0x7f800000u) == 0x7f800000u || (sizeof(T) == 2 && (most & 0x7f80u) == 0x7f80u);
+}
 
 // Replaces non-finite elements of a chunk by zero; true if there was one.
 template <typename T> __device__ __forceinline__ bool clean_chunk(u32x4& v)
@@ -231,14 +277,20 @@ __device__ __forceinline__ void second_product(f32x4 (&acc)[DP / 16], const f32x
             const u32x4 b = {pack_bf16x2(w[2 * tp][0], w[2 * tp][1]), pack_bf16x2(w[2 * tp][2], w[2 * tp][3]),
                              pack_bf16x2(w[2 * tp + 1][0], w[2 * tp + 1][1]), pack_bf16x2(w[2 * tp + 1][2], w[2 * tp + 1][3])};
 #pragma unroll
-            for (int dt = 0; dt < S::DT; ++dt) acc[dt] = mma<T>(rd.col_frag2(tile, tp, dt), b, acc[dt]);
+            for (int dt = 0; dt < S::DT; ++dt) {
+                acc[dt] = mma<T>(rd.col_frag2(tile, tp, dt), b, acc[dt]);
+                if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
         }
     } else {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const u32x4 b = __builtin_bit_cast(u32x4, w[t]);
 #pragma unroll
-            for (int dt = 0; dt < S::DT; ++dt) acc[dt] = mma<T>(rd.col_frag1(tile, t, dt), b, acc[dt]);
+            for (int dt = 0; dt < S::DT; ++dt) {
+                acc[dt] = mma<T>(rd.col_frag1(tile, t, dt), b, acc[dt]);
+                if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
         }
     }
 }
@@ -254,6 +306,7 @@ __device__ __forceinline__ void first_product(f32x4 (&first)[4], const u32x4 (&o
         first[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kk = 0; kk < S::KK; ++kk) first[t] = mma<T>(rd.row_frag(tile, t, kk), own[kk], first[t]);
+        if (S::KK >= 4 || t % 2) __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -361,27 +414,272 @@ __device__ __forceinline__ float tanh_f32(float x)
     return fabsf(x) < 0.4f ? s : far;
 }
 
-__device__ __forceinline__ int bucket_side(const AttBuckets& bk, int n)
+// A tile's products to scores in units of log 2: scaled, capped, with the bias `flat2` of the whole tile; slope (capped
+// scores only): d score / d product over the scale.  The groups are kept apart, or the compiler works on all 16 at once and runs
+// out of registers.
+template <bool CAP>
+__device__ __forceinline__ void to_scores(f32x4 (&s)[4], f32x4 (&slope)[CAP ? 4 : 1], float zc, float cap2, float z2, float flat2)
 {
-    if (n < bk.exact) return n;
-    int b = bk.exact;
-    for (int i = 0; i < bk.borders; ++i) b += n >= bk.border[i];
-    return b;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if constexpr (CAP) {
+                const float th = tanh_f32(s[n][r] * zc);
+                slope[n][r] = 1.f - th * th;
+                s[n][r] = th * cap2 + flat2;
+            } else {
+                s[n][r] = s[n][r] * z2 + flat2;
+            }
+        }
+        if constexpr (CAP) __builtin_amdgcn_sched_barrier(0);
+    }
 }
-__device__ __forceinline__ int bucket_of(const AttBuckets& bk, int n)
+
+// border: the borders in LDS.  The logarithm gives the bucket or one beside it.
+__device__ __forceinline__ int bucket_side(const AttBuckets& bk, const int* border, int n)
 {
-    if (n >= 0) return bucket_side(bk, n);
-    return bk.two_sided ? bk.side + bucket_side(bk, -n) : 0;
+    int i = (int)(__builtin_amdgcn_logf((float)n * bk.inv_exact) * bk.per_log2);
+    i = i < 0 ? 0 : i > bk.borders ? bk.borders : i;
+    const int below = border[i > 0 ? i - 1 : 0], above = border[i];
+    if (i > 0 && n < below) --i;
+    else if (i < bk.borders && n >= above) ++i;
+    return n < bk.exact ? n : bk.exact + i;
+}
+__device__ __forceinline__ int bucket_of(const AttBuckets& bk, const int* border, int n)
+{
+    const int b = bucket_side(bk, border, n < 0 ? -n : n);
+    return n >= 0 ? b : bk.two_sided ? bk.side + b : 0;
 }
 // The one bucket of all distances in [lo, hi], or -1 (several, or not looked for).
 __device__ __forceinline__ int uniform_bucket(const AttBuckets& bk, int lo, int hi)
 {
-    const int last = bk.borders ? bk.border[bk.borders - 1] : bk.exact;      // from here on: bucket side - 1
-    if (lo >= last) return bk.side - 1;
+    if (lo >= bk.last) return bk.side - 1;
     if (hi < 0 && !bk.two_sided) return 0;
-    if (-hi >= last && hi < 0) return 2 * bk.side - 1;
+    if (hi < 0 && -hi >= bk.last) return 2 * bk.side - 1;
     return -1;
 }
+
+// ---- walking the streamed rows ----------------------------------------------------------------------------
+
+// Work item of a block: the blocks of one head of one history share its rows, so neighbours in this order go to one XCD
+// (blocks are dealt to the 8 XCDs in turn).
+__device__ __forceinline__ int xcd_item(int items)
+{
+    const int each = (items + 7) / 8;
+    const int item = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
+    return (int)(blockIdx.x >> 3) < each && item < items ? item : -1;
+}
+
+__device__ __forceinline__ int row_segment(const int* __restrict__ seg, int row, int length)
+{
+    if (row >= length) return kNoSeg;
+    const int v = seg ? seg[row] : 0;
+    return v < 0 ? kNoSeg : v;
+}
+
+struct TileMarks {
+    uint32_t active[kAttMaxTiles / 32], mixed[kAttMaxTiles / 32];
+    int red[12];
+};
+
+// Marks the tiles [t0, t1) of streamed rows that hold a row of a segment in the owner rows' range, and among them those
+// with any row that is not of the one segment all owner rows have.  own: this lane's segment of its owner row, if there.
+__device__ __forceinline__ void mark_tiles(TileMarks& mk, const int* __restrict__ seg, int length, int own, bool there, int t0, int t1)
+{
+    int lo = there && own >= 0 ? own : 0x7fffffff, hi = there && own >= 0 ? own : -1;
+    lo = wave_min(lo), hi = wave_max_i(hi);
+    int bad = __any(there && own < 0);
+    if (lane_id() == 0) mk.red[wave_id()] = lo, mk.red[4 + wave_id()] = hi, mk.red[8 + wave_id()] = bad;
+    for (int i = t0 / 32 + threadIdx.x; i <= t1 / 32; i += kBlock)
+        if (i < kAttMaxTiles / 32) mk.active[i] = 0u, mk.mixed[i] = 0u;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWavesPerBlock; ++w) {
+        lo = mk.red[w] < lo ? mk.red[w] : lo;
+        hi = mk.red[4 + w] > hi ? mk.red[4 + w] : hi;
+        bad |= mk.red[8 + w];
+    }
+    const bool one = lo == hi && !bad;
+    for (int t = t0 + wave_id(); t < t1; t += kWavesPerBlock) {
+        const int v = row_segment(seg, t * kTile + lane_id(), length);
+        const bool touch = __any(v >= lo && v <= hi);
+        const bool plain = one && __all(v == lo);
+        if (lane_id() == 0) {
+            if (touch) atomicOr(&mk.active[t >> 5], 1u << (t & 31));
+            if (!plain) atomicOr(&mk.mixed[t >> 5], 1u << (t & 31));
+        }
+    }
+    __syncthreads();
+}
+
+// mk NULL: every tile is active and none is mixed.
+__device__ __forceinline__ int next_tile(int t, int t1, const TileMarks* mk)
+{
+    if (mk)
+        while (t < t1) {
+            const uint32_t rest = mk->active[t >> 5] >> (t & 31);
+            if (rest) {
+                t += __builtin_ctz(rest);
+                break;
+            }
+            t = (t | 31) + 1;
+        }
+    return __builtin_amdgcn_readfirstlane(t < t1 ? t : t1);
+}
+__device__ __forceinline__ bool tile_mixed(const TileMarks* mk, int t)
+{
+    return mk && __builtin_amdgcn_readfirstlane((mk->mixed[t >> 5] >> (t & 31)) & 1);
+}
+
+// The streamed operands: a tile of each, loaded to registers while the tile before is worked on, then written to LDS.
+template <typename T, int DP, int UNIT> struct Feed {
+    using S = Shape<T, DP>;
+    static constexpr int STEP = kBlock / S::NCH;      // rows between a thread's chunks
+    u32x4 a[S::NC], b[S::NC];
+    int seg;                                          // of row (lane) of the tile
+
+    // pa, pb: row row0 of the operands
+    __device__ __forceinline__ void load(const T* pa, int64_t sa, const T* pb, int64_t sb, int row0, int length,
+                                         const int* __restrict__ segments, int dim)
+    {
+        const RowSource ra = row_source(pa, sa, length - row0, dim), rb = row_source(pb, sb, length - row0, dim);
+        const uint32_t row = threadIdx.x / S::NCH;
+        const int ch = threadIdx.x % S::NCH;
+#pragma unroll
+        for (int i = 0; i < S::NC; ++i) {
+            a[i] = load_chunk<T, UNIT>(ra, (row + i * STEP) * ra.stride, ch, dim);
+            b[i] = load_chunk<T, UNIT>(rb, (row + i * STEP) * rb.stride, ch, dim);
+        }
+        seg = row_segment(segments, row0 + lane_id(), length);
+    }
+    // guard: pairs of the tile are masked, so a non-finite element would reach rows that do not see it.  CAREFUL: they are
+    // replaced by zeros in the operands named (those that enter a second product) and flagged; else only flagged.
+    template <bool CAREFUL, bool A, bool B>
+    __device__ __forceinline__ void put(unsigned char* ta, unsigned char* tb, int* s_seg, bool guard, bool odd, uint32_t* flags)
+    {
+        const int row = threadIdx.x / S::NCH, ch = threadIdx.x % S::NCH;
+        const uint64_t there = __ballot(seg != kNoSeg);
+        if (~there) {                                 // padding contributes nothing, whatever it holds
+#pragma unroll
+            for (int i = 0; i < S::NC; ++i)
+                if (!((there >> (row + i * STEP)) & 1)) a[i] = b[i] = u32x4{0u, 0u, 0u, 0u};
+        }
+        if (guard) {
+            if constexpr (CAREFUL) {
+#pragma unroll
+                for (int i = 0; i < S::NC; ++i) {
+                    if (A) odd |= clean_chunk<T>(a[i]);
+                    if (B) odd |= clean_chunk<T>(b[i]);
+                }
+            } else {
+                uint32_t most = 0u;
+#pragma unroll
+                for (int i = 0; i < S::NC; ++i) most = max_exponent<T>(max_exponent<T>(most, a[i]), b[i]);
+                odd |= has_nonfinite<T>(most);
+            }
+            odd = __any(odd);
+            if (lane_id() == 0) flags[wave_id()] = odd;
+        } else if (CAREFUL && lane_id() == 0) {
+            flags[wave_id()] = 0u;
+        }
+        if (wave_id() == 0) s_seg[lane_id()] = seg;
+#pragma unroll
+        for (int i = 0; i < S::NC; ++i) {
+            const int at = (row + i * STEP) * S::RB + ((ch ^ swz<S::NCH>(row + i * STEP)) * 16);
+            *reinterpret_cast<u32x4*>(ta + at) = a[i];
+            *reinterpret_cast<u32x4*>(tb + at) = b[i];
+        }
+    }
+};
+
+__device__ __forceinline__ bool any_flag(const uint32_t* flags)
+{
+    const u32x4 f = *reinterpret_cast<const u32x4*>(flags);
+    return __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]) != 0;
+}
+
+// A tile's masked scores: minus infinity where !(row of the tile in the owner's segment and below `last` [from `first` on]).
+// SEGMENTS: compare the rows' segments, else only their place.
+template <bool SEGMENTS>
+__device__ __forceinline__ uint32_t visible_bits(const int* s_seg, int own, int first, int last)
+{
+    const int g4 = 4 * (lane_id() >> 4);
+    uint32_t vis = 0u;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        i32x4 sg = {0, 0, 0, 0};
+        if (SEGMENTS) sg = *reinterpret_cast<const i32x4*>(s_seg + 16 * n + g4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const bool see = (!SEGMENTS || sg[r] == own) && 16 * n + r < last - g4 && 16 * n + r >= first - g4;
+            vis |= see ? 1u << (4 * n + r) : 0u;
+        }
+    }
+    return vis;
+}
+template <bool SEGMENTS, bool FROM>
+__device__ __forceinline__ void mask_scores(f32x4 (&s)[4], const int* s_seg, int own, int edge)
+{
+    const int g4 = 4 * (lane_id() >> 4);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        i32x4 sg = {0, 0, 0, 0};
+        if (SEGMENTS) sg = *reinterpret_cast<const i32x4*>(s_seg + 16 * n + g4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const bool see = (!SEGMENTS || sg[r] == own) && (FROM ? 16 * n + r >= edge - g4 : 16 * n + r < edge - g4);
+            s[n][r] = see ? s[n][r] : -INFINITY;
+        }
+    }
+}
+
+// Owner fragments: row c of the wave's 16, zeros where the row is padding or not there.
+template <typename T, int DP, int UNIT>
+__device__ __forceinline__ void load_owner(u32x4 (&f)[DP * sizeof(T) / 64], const T* base, int64_t sr, int rows, int dim, bool live)
+{
+    const RowSource src = row_source(base, sr, rows < 16 ? rows : 16, dim);
+    const int c = lane_id() & 15, g = lane_id() >> 4;
+#pragma unroll
+    for (int kk = 0; kk < Shape<T, DP>::KK; ++kk) {
+        f[kk] = load_chunk<T, UNIT>(src, (uint32_t)c * src.stride, g + 4 * kk, dim);
+        if (!live) f[kk] = u32x4{0u, 0u, 0u, 0u};
+    }
+}
+
+// ---- launches ---------------------------------------------------------------------------------------------
+// unit: bytes per global access (template argument UNIT): 16, 8 (bf16 only), or the size of an element
+template <typename F> inline void by_shape(const gram_attention_config& c, int unit, F&& go)
+{
+    auto width = [&](auto type, auto u) {
+        if (c.head_dim <= 32) go(type, std::integral_constant<int, 32>{}, u);
+        else if (c.head_dim <= 64) go(type, std::integral_constant<int, 64>{}, u);
+        else go(type, std::integral_constant<int, 128>{}, u);
+    };
+    if (c.dtype == GRAM_BF16) {
+        if (unit == 16) width(Bf16{}, std::integral_constant<int, 16>{});
+        else if (unit == 8) width(Bf16{}, std::integral_constant<int, 8>{});
+        else width(Bf16{}, std::integral_constant<int, 2>{});
+    } else {
+        if (unit == 16) width(float{}, std::integral_constant<int, 16>{});
+        else width(float{}, std::integral_constant<int, 4>{});
+    }
+}
+template <typename F> inline void by_shape_and_cap(const gram_attention_config& c, int unit, F&& go)
+{
+    by_shape(c, unit, [&](auto type, auto dp, auto u) {
+        if (c.cap > 0.f) go(type, dp, u, std::true_type{});
+        else go(type, dp, u, std::false_type{});
+    });
+}
+inline dim3 att_grid(int items) { return dim3((unsigned)((items + 7) / 8 * 8)); }
+constexpr int att_blocks(int length, int rows) { return (length + rows - 1) / rows; }
+
+void attend_forward(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s);      // gram_attend_fwd.hip
+void attend_backward_queries(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s);     // gram_attend_dq.hip
+void attend_backward_keys(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s);        // gram_attend_dkv.hip
 
 // ---- gram_attend_step.hip ---------------------------------------------------------------------------------
 int64_t step_part_bytes(const gram_attention_config& c, int32_t batch, int32_t capacity);

@@ -1,0 +1,327 @@
+// Attention over item histories, backward pass over the queries: dq and the gradient of the table (notation of
+// gram_attend_fwd.hip).
+//
+//   dp_ij = do_i.v_j   delta_i = sum_j p_ij dp_ij   ds_ij = p_ij (dp_ij - delta_i)   dz_ij = ds_ij (1 - (c_ij / cap)^2)
+//   dq_i = scale sum_j dz_ij k_j       dtable[head, b] = sum of ds over the pairs of bucket b
+//
+// delta is do.o where only dq, dk and dv are asked for, whose own rounding is as coarse as that of o.  The table's gradient
+// is float32, sums over whole batches in which an error of delta does not average out: for it a first walk over the keys
+// sums p dp in float32.
+#include "gram_attend.h"
+
+namespace gram {
+
+namespace {
+
+constexpr int kNear = 383;       // distances that have a sum of their own
+constexpr int kStrip = 92;       // distances of a wave's 16 queries and a tile's 64 keys, each group's row of them
+
+template <typename T, int DP> struct DqShared {
+    __attribute__((aligned(1024))) unsigned char k[Shape<T, DP>::TILE], v[Shape<T, DP>::TILE];
+    __attribute__((aligned(16))) int seg[kTile];
+    __attribute__((aligned(16))) uint32_t flags[4];
+    float bias[2 * kTile];
+    float table[kMaxBorders];
+    int border[kMaxBorders];
+    float strip[kWavesPerBlock][4][kStrip];        // see table_near
+    float bucket[kWavesPerBlock][kMaxBorders];     // sums of ds by bucket, each wave's own
+    TileMarks marks;
+};
+
+// The table's gradient.  A tile of one bucket adds its ds to a register of each lane.  A tile of several adds along its
+// diagonals, which are the distances: lane (c, g) holds queries c and keys 16 n + 4 g + r, distance (a number of the tile)
+// + c - 4 g - r - 16 n.  Shifting the registers r = 1..3 by r lanes within their row of 16 brings equal distances
+// together; what is shifted out belongs to the same lanes' distances of n + 1.  That leaves five values a lane, distance
+// + c - 4 g - 16 n, n = 0..4; the four groups are joined through LDS, where the sum of a distance is added to the wave's
+// own `dist` row (distances within kNear) or, farther out where buckets are wide, bucket by bucket.  No word has two
+// writers, so every sum has one order.
+template <int SHIFT> __device__ __forceinline__ float row_shift(float v)        // lane i gets lane i + SHIFT's, 0 from outside
+{
+    constexpr int CTRL = SHIFT > 0 ? 0x100 | SHIFT : 0x110 | -SHIFT;            // row_shl, row_shr
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+
+__device__ __forceinline__ void add_bucket(float* bucket, int b, float lane_sums)
+{
+    const float sum = wave_total(lane_sums);
+    if (lane_id() == 0) bucket[b] += sum;
+}
+
+// top: the distance of the wave's first query and the tile's first key.
+__device__ __forceinline__ void table_near(const AttArgs& a, const f32x4 (&ds)[4], int top, float (*strip)[kStrip], float* dist,
+                                           float* bucket, const int* border)
+{
+    const int c = lane_id() & 15, g = lane_id() >> 4;
+    float spill = 0.f;
+    // distance top + c - 4 g - 16 n lies at place c - 4 g - 16 n + 76 of its group's row
+    float* const at = &strip[g][c - 4 * g + 76];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        at[-16 * n] = ds[n][0] + row_shift<1>(ds[n][1]) + row_shift<2>(ds[n][2]) + row_shift<3>(ds[n][3]) + spill;
+        spill = row_shift<-15>(ds[n][1]) + row_shift<-14>(ds[n][2]) + row_shift<-13>(ds[n][3]);
+    }
+    at[-64] = spill;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    float sum[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int place = lane_id() + 64 * h;
+        sum[h] = 0.f;
+        if (place < kStrip) sum[h] = (strip[0][place] + strip[1][place]) + (strip[2][place] + strip[3][place]);
+    }
+    __builtin_amdgcn_wave_barrier();
+    const int n0 = top - 76;                                   // distance of place 0
+    if (n0 >= -kNear && n0 + kStrip - 1 <= kNear) {
+        dist[n0 + lane_id()] += sum[0];
+        if (lane_id() + 64 < kStrip) dist[n0 + 64 + lane_id()] += sum[1];
+    } else {
+        const int b0 = bucket_of(a.bk, border, n0 + lane_id()), b1 = bucket_of(a.bk, border, n0 + 64 + lane_id());
+        uint64_t left0 = ~0ull, left1 = __ballot(lane_id() + 64 < kStrip);
+        while (left0 | left1) {
+            const int b = left0 ? __builtin_amdgcn_readlane(b0, __builtin_ctzll(left0)) : __builtin_amdgcn_readlane(b1, __builtin_ctzll(left1));
+            const bool m0 = b0 == b, m1 = lane_id() + 64 < kStrip && b1 == b;
+            add_bucket(bucket, b, (m0 ? sum[0] : 0.f) + (m1 ? sum[1] : 0.f));
+            left0 &= ~__ballot(m0), left1 &= ~__ballot(m1);
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// One block: 64 queries of one head; false as for attend_block.  dist: kWavesPerBlock rows of 2 kNear + 1 sums of ds by
+// distance.
+template <typename T, int DP, int UNIT, bool CAP, bool CAREFUL>
+__device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, float* dist, int item)
+{
+    using S = Shape<T, DP>;
+    const int nqt = (a.length + kTile - 1) / kTile;
+    const int qt = nqt - 1 - item % nqt;
+    const int head = (item / nqt) % a.heads, batch = item / nqt / a.heads, kvh = head / a.group;
+    const int c = lane_id() & 15, g = lane_id() >> 4;
+    const int q0 = qt * kTile, wq0 = q0 + wave_id() * 16, q = wq0 + c;
+    const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
+    const int prefix = a.prefix ? a.prefix[batch] : 0;
+    const T* const kp = static_cast<const T*>(a.k.data) + batch * a.k.sb + kvh * a.k.sh;
+    const T* const vp = static_cast<const T*>(a.v.data) + batch * a.v.sb + kvh * a.v.sh;
+    const int64_t stat = ((int64_t)batch * a.heads + head) * a.length + (q < a.length ? q : a.length - 1);
+    const bool want_table = a.part != nullptr;
+
+    u32x4 qf[S::KK], df[S::KK];
+    const int qseg = q < a.length ? row_segment(seg, q, a.length) : kNoSegOwner;
+    const bool live = qseg >= 0;
+    load_owner<T, DP, UNIT>(qf, static_cast<const T*>(a.q.data) + batch * a.q.sb + head * a.q.sh + wq0 * a.q.sr, a.q.sr,
+                            a.length - wq0, a.dim, live);
+    load_owner<T, DP, UNIT>(df, static_cast<const T*>(a.dout.data) + batch * a.dout.sb + head * a.dout.sh + wq0 * a.dout.sr,
+                            a.dout.sr, a.length - wq0, a.dim, live);
+    float delta = 0.f;
+    if (!want_table) {
+        u32x4 of[S::KK];
+        load_owner<T, DP, UNIT>(of, static_cast<const T*>(a.o.data) + batch * a.o.sb + head * a.o.sh + wq0 * a.o.sr, a.o.sr,
+                                a.length - wq0, a.dim, live);
+#pragma unroll
+        for (int kk = 0; kk < S::KK; ++kk) delta += dot_chunk<T>(df[kk], of[kk]);
+        delta = group_sum(delta);
+    }
+    const float lse = a.lse[stat];
+    const float lse2 = lse == -INFINITY ? 0.f : lse * kLog2e;     // a row that sees nothing: all its pairs are masked
+    const int own = live ? qseg : kNoSegOwner;
+    const int ntiles = (a.length + kTile - 1) / kTile;
+    int t1 = ntiles;
+    if (a.causal) {
+        t1 = qt + 1;
+        const int pt = (prefix + kTile - 1) / kTile;
+        t1 = pt > t1 ? pt : t1;
+        t1 = t1 < ntiles ? t1 : ntiles;
+    }
+    const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
+    if ((int)threadIdx.x < buckets) sh.table[threadIdx.x] = a.table[(int64_t)head * buckets + threadIdx.x] * kLog2e;
+    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = a.bk.border[threadIdx.x];
+    if (want_table) {
+        for (int i = threadIdx.x; i < kWavesPerBlock * (2 * kNear + 1); i += kBlock) dist[i] = 0.f;
+        for (int i = threadIdx.x; i < kWavesPerBlock * 4 * kStrip; i += kBlock) (&sh.strip[0][0][0])[i] = 0.f;
+        if (threadIdx.x < kMaxBorders)
+            for (int w = 0; w < kWavesPerBlock; ++w) sh.bucket[w][threadIdx.x] = 0.f;
+    }
+    float* const my_dist = dist + wave_id() * (2 * kNear + 1) + kNear;
+    if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
+    const TileMarks* const mk = seg ? &sh.marks : nullptr;
+
+    const Reader<T, DP> rd;
+    Feed<T, DP, UNIT> feed;
+    f32x4 dq[S::DT];
+#pragma unroll
+    for (int dt = 0; dt < S::DT; ++dt) dq[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float z2 = a.scale * kLog2e, zc = CAP ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
+    int last = a.length;
+    if (a.causal) {
+        last = q + 1 > prefix ? q + 1 : prefix;
+        last = last < a.length ? last : a.length;
+    }
+    if (q >= a.length) last = 0;                                  // the table's gradient is summed over rows
+    const bool full_rows = wq0 + 16 <= a.length;
+    int flat_bucket = -1;
+    float flat_sum = 0.f;
+
+    auto whole = [&](int t, int row, bool mixed) {
+        const int k1 = t * kTile + kTile;
+        return !mixed && k1 <= a.length && (!a.causal || k1 - 1 <= row || k1 <= prefix);
+    };
+    auto load = [&](int t) {
+        const int k0 = t * kTile;
+        feed.load(kp + k0 * a.k.sr, a.k.sr, vp + k0 * a.v.sr, a.v.sr, k0, a.length, seg, a.dim);
+    };
+
+    // DELTA: only sum p dp; else the gradients, with that sum on the way where the one tile holds it all
+    const int tfirst = next_tile(0, t1, mk);
+    const bool one_tile = want_table && next_tile(tfirst + 1, t1, mk) >= t1;
+    auto walk = [&](auto delta_only) -> bool {
+        constexpr bool DELTA = decltype(delta_only)::value;
+        int t = tfirst;
+        if (t < t1) load(t);
+        while (t < t1) {
+            const bool mixed = tile_mixed(mk, t);
+            const bool guard = !whole(t, q0, mixed);
+            const int k0 = t * kTile, hi = q0 + kTile - 1 - k0;
+            const int flat = a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
+            __syncthreads();
+            feed.template put<CAREFUL, true, false>(sh.k, sh.v, sh.seg, guard, false, sh.flags);
+            if (flat < 0 && (int)threadIdx.x < 2 * kTile - 1) {
+                sh.bias[threadIdx.x] = sh.table[bucket_of(a.bk, sh.border, hi - (int)threadIdx.x)];
+            }
+            const int tn = next_tile(t + 1, t1, mk);
+            if (tn < t1) load(tn);
+            __syncthreads();
+            const bool odd = (CAREFUL || guard) && any_flag(sh.flags);
+            if (!CAREFUL && odd) return false;
+            if (wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix)) {
+                f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
+                first_product<T, DP>(s, qf, rd, sh.k);
+                const float flat2 = a.bk.side && flat >= 0 ? sh.table[flat] : 0.f;
+                to_scores<CAP>(s, slope, zc, cap2, z2, flat2);
+                if (flat < 0) {
+                    const float* const bias = &sh.bias[4 * g - (q - q0) + kTile - 1];
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[n][r] += bias[16 * n + r];
+                }
+                uint32_t vis = 0xffffu;
+                if (!whole(t, wq0, mixed) || !full_rows) {
+                    if (CAREFUL && odd) vis = visible_bits<true>(sh.seg, own, 0, last - k0);
+                    if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0);
+                    else mask_scores<false, false>(s, sh.seg, own, last - k0);
+                }
+                first_product<T, DP>(dp, df, rd, sh.v);
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - lse2);
+                        // a masked pair has weight 0; its dp may be anything
+                        if (CAREFUL && !((vis >> (4 * n + r)) & 1)) dp[n][r] = 0.f;
+                    }
+                if (DELTA || one_tile) {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) delta += s[n][r] * dp[n][r];
+                }
+                if constexpr (!DELTA) {
+                    if (one_tile) delta = group_sum(delta);
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[n][r] *= dp[n][r] - delta;
+                    if (want_table) {
+                        if (flat >= 0) {
+                            if (flat != flat_bucket) {
+                                if (flat_bucket >= 0) add_bucket(sh.bucket[wave_id()], flat_bucket, flat_sum);
+                                flat_bucket = flat, flat_sum = 0.f;
+                            }
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) flat_sum += (s[n][0] + s[n][1]) + (s[n][2] + s[n][3]);
+                        } else {
+                            table_near(a, s, wq0 - k0, sh.strip[wave_id()], my_dist, sh.bucket[wave_id()], sh.border);
+                        }
+                    }
+                    if constexpr (CAP) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) s[n] *= slope[n];
+                    }
+                    second_product<T, DP>(dq, s, rd, sh.k);
+                    if (CAREFUL && odd) add_nonfinite<T, DP>(dq, s, vis, kp + k0 * a.k.sr, a.k.sr, a.length - k0, a.dim);
+                }
+            }
+            t = tn;
+        }
+        if constexpr (DELTA) delta = group_sum(delta);
+        return true;
+    };
+    if (want_table && !one_tile && !walk(std::true_type{})) return false;
+    if (!walk(std::false_type{})) return false;
+
+    if (q < a.length) {
+        T* const dqp = static_cast<T*>(a.dq.data) + batch * a.dq.sb + head * a.dq.sh + q * a.dq.sr;
+#pragma unroll
+        for (int dt = 0; dt < S::DT; ++dt) store4<T, UNIT>(dqp, 16 * dt + 4 * g, a.dim, dq[dt] * a.scale);
+        if (g == 0) a.delta[stat] = delta;
+    }
+    if (want_table) {
+        if (flat_bucket >= 0) add_bucket(sh.bucket[wave_id()], flat_bucket, flat_sum);
+        __syncthreads();
+        // bucket b of a side: the distances from its border to the next one's; keys after the query count as distance 0
+        // where there is one side
+        for (int b = wave_id(); b < buckets; b += kWavesPerBlock) {
+            const bool after = b >= a.bk.side;
+            const int i = (after ? b - a.bk.side : b) - a.bk.exact;
+            int from = i < 0 ? i + a.bk.exact : i == 0 ? a.bk.exact : sh.border[i - 1];
+            int to = i < 0 ? from + 1 : i < a.bk.borders ? sh.border[i] : kNear + 1;
+            to = to < kNear + 1 ? to : kNear + 1;
+            if (after && from == 0) from = 1;
+            const float* const row = dist + kNear;
+            constexpr int W = 2 * kNear + 1;
+            float sum = lane_id() < kWavesPerBlock ? sh.bucket[lane_id()][b] : 0.f;
+            for (int n = from + lane_id(); n < to; n += kWave) {
+                const float* const r = row + (after ? -n : n);
+                sum += (r[0] + r[W]) + (r[2 * W] + r[3 * W]);
+            }
+            if (b == 0 && !a.bk.two_sided)
+                for (int n = 1 + lane_id(); n <= 2 * kTile; n += kWave) sum += (row[-n] + row[W - n]) + (row[2 * W - n] + row[3 * W - n]);
+            sum = wave_total(sum);
+            if (lane_id() == 0) a.part[((int64_t)head * a.parts + batch * nqt + qt) * buckets + b] = sum;
+        }
+    }
+    return true;
+}
+
+template <typename T, int DP, int UNIT, bool CAP>
+__device__ __noinline__ void dq_block_careful(const AttArgs& a, DqShared<T, DP>& sh, float* dist, int item)
+{
+    __syncthreads();
+    dq_block<T, DP, UNIT, CAP, true>(a, sh, dist, item);
+}
+
+template <typename T, int DP, int UNIT, bool CAP, int WAVES>
+__global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
+{
+    extern __shared__ float s_dist[];
+    __shared__ DqShared<T, DP> sh;
+    const int item = xcd_item(a.items);
+    if (item < 0) return;
+    if (!dq_block<T, DP, UNIT, CAP, false>(a, sh, s_dist, item)) dq_block_careful<T, DP, UNIT, CAP>(kernel_args(), sh, s_dist, item);
+}
+
+}  // namespace
+
+void attend_backward_queries(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s)
+{
+    a.items = a.batch * a.heads * att_blocks(a.length, kTile);
+    const size_t dist = a.part ? kWavesPerBlock * (2 * kNear + 1) * sizeof(float) : 0;
+    by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
+        constexpr int DP = decltype(dp)::value;
+        constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 3 : 2;
+        k_attend_dq<decltype(type), DP, decltype(u)::value, decltype(cap)::value, WAVES><<<att_grid(a.items), dim3(kBlock), dist, s>>>(a);
+    });
+}
+
+}  // namespace gram

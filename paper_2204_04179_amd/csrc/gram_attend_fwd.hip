@@ -1,0 +1,185 @@
+// Attention over item histories, forward.
+//
+//   z_ij = scale q_i.k_j    c_ij = cap tanh(z_ij / cap) or z_ij    s_ij = c_ij + table[head, bucket(i - j)]
+//   visible(i, j):  segment_i = segment_j >= 0  and  (not causal or j <= i or j < prefix)
+//   o_i = sum_j p_ij v_j,  p_ij = exp(s_ij - lse_i) over the visible j
+//
+// One pass over the keys with the running maximum and sum of the softmax; scores and weights stay in registers.
+#include "gram_attend.h"
+
+namespace gram {
+
+namespace {
+
+template <typename T, int DP> struct FwdShared {
+    __attribute__((aligned(1024))) unsigned char k[Shape<T, DP>::TILE], v[Shape<T, DP>::TILE];
+    __attribute__((aligned(16))) int seg[kTile];
+    __attribute__((aligned(16))) uint32_t flags[4];
+    float bias[2 * kTile];
+    float table[kMaxBorders];
+    int border[kMaxBorders];
+    TileMarks marks;
+};
+
+// One block: 64 queries of one head, 16 to a wave.  False (CAREFUL not set): a tile with masked pairs holds a non-finite
+// element, nothing has been written, and the block starts again with the careful form.  Apart, so that the registers of the
+// rare form are not the common one's.
+template <typename T, int DP, int UNIT, bool CAP, bool CAREFUL>
+__device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>& sh, int item)
+{
+    using S = Shape<T, DP>;
+    const int nqt = (a.length + kTile - 1) / kTile;
+    const int qt = nqt - 1 - item % nqt;                 // the longest rows of a causal mask first
+    const int head = (item / nqt) % a.heads, batch = item / nqt / a.heads, kvh = head / a.group;
+    const int c = lane_id() & 15, g = lane_id() >> 4;
+    const int q0 = qt * kTile, wq0 = q0 + wave_id() * 16, q = wq0 + c;
+    const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
+    const int prefix = a.prefix ? a.prefix[batch] : 0;
+    const T* const kp = static_cast<const T*>(a.k.data) + batch * a.k.sb + kvh * a.k.sh;
+    const T* const vp = static_cast<const T*>(a.v.data) + batch * a.v.sb + kvh * a.v.sh;
+
+    u32x4 qf[S::KK];
+    const int qseg = q < a.length ? row_segment(seg, q, a.length) : kNoSegOwner;
+    load_owner<T, DP, UNIT>(qf, static_cast<const T*>(a.q.data) + batch * a.q.sb + head * a.q.sh + wq0 * a.q.sr, a.q.sr,
+                            a.length - wq0, a.dim, qseg >= 0);
+    const int own = qseg < 0 ? kNoSegOwner : qseg;
+    const int ntiles = (a.length + kTile - 1) / kTile;
+    int t1 = ntiles;
+    if (a.causal) {
+        t1 = qt + 1;
+        const int pt = (prefix + kTile - 1) / kTile;
+        t1 = pt > t1 ? pt : t1;
+        t1 = t1 < ntiles ? t1 : ntiles;
+    }
+    const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
+    if ((int)threadIdx.x < buckets) sh.table[threadIdx.x] = a.table[(int64_t)head * buckets + threadIdx.x] * kLog2e;
+    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = a.bk.border[threadIdx.x];
+    if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
+    const TileMarks* const mk = seg ? &sh.marks : nullptr;
+
+    const Reader<T, DP> rd;
+    Feed<T, DP, UNIT> feed;
+    f32x4 o[S::DT];
+    float top = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < S::DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float z2 = a.scale * kLog2e, zc = CAP ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
+    int last = a.length;                                 // keys before it are in sight, segments aside
+    if (a.causal) {
+        last = q + 1 > prefix ? q + 1 : prefix;
+        last = last < a.length ? last : a.length;
+    }
+
+    // whether all pairs of the tile with rows from `row` on are visible
+    auto whole = [&](int t, int row, bool mixed) {
+        const int k1 = t * kTile + kTile;
+        return !mixed && k1 <= a.length && (!a.causal || k1 - 1 <= row || k1 <= prefix);
+    };
+    auto load = [&](int t) {
+        const int k0 = t * kTile;
+        feed.load(kp + k0 * a.k.sr, a.k.sr, vp + k0 * a.v.sr, a.v.sr, k0, a.length, seg, a.dim);
+    };
+
+    int t = next_tile(0, t1, mk);
+    if (t < t1) load(t);
+    while (t < t1) {
+        const bool mixed = tile_mixed(mk, t);
+        const bool guard = !whole(t, q0, mixed);
+        const int k0 = t * kTile, hi = q0 + kTile - 1 - k0;       // the largest distance of the block's pairs
+        const int flat = a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
+        __syncthreads();                                          // the tile before has been read
+        feed.template put<CAREFUL, false, true>(sh.k, sh.v, sh.seg, guard, false, sh.flags);
+        if (flat < 0 && (int)threadIdx.x < 2 * kTile - 1)
+            sh.bias[threadIdx.x] = sh.table[bucket_of(a.bk, sh.border, hi - (int)threadIdx.x)];
+        const int tn = next_tile(t + 1, t1, mk);
+        if (tn < t1) load(tn);
+        __syncthreads();
+        const bool odd = (CAREFUL || guard) && any_flag(sh.flags);
+        if (!CAREFUL && odd) return false;
+        if (wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix)) {
+            f32x4 s[4], slope[CAP ? 4 : 1];
+            first_product<T, DP>(s, qf, rd, sh.k);
+            const float flat2 = a.bk.side && flat >= 0 ? sh.table[flat] : 0.f;
+            to_scores<CAP>(s, slope, zc, cap2, z2, flat2);
+            if (flat < 0) {
+                const float* const bias = &sh.bias[4 * g - (q - q0) + kTile - 1];
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[n][r] += bias[16 * n + r];
+            }
+            uint32_t vis = 0xffffu;
+            if (!whole(t, wq0, mixed)) {
+                if (CAREFUL && odd) vis = visible_bits<true>(sh.seg, own, 0, last - k0);
+                if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0);
+                else mask_scores<false, false>(s, sh.seg, own, last - k0);
+            }
+            float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+#pragma unroll
+            for (int n = 1; n < 4; ++n) mx = fmaxf(mx, fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])));
+            mx = group_max(mx);
+            if (__any(mx > top)) {
+                const float nt = fmaxf(mx, top);
+                const float shrink = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - nt);
+                top = nt;
+                total *= shrink;
+#pragma unroll
+                for (int dt = 0; dt < S::DT; ++dt) o[dt] *= shrink;
+            }
+            const float base = top == -INFINITY ? 0.f : top;      // a row that has seen nothing so far
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - base);
+                    total += s[n][r];
+                }
+            second_product<T, DP>(o, s, rd, sh.v);
+            if (CAREFUL && odd) add_nonfinite<T, DP>(o, s, vis, vp + k0 * a.v.sr, a.v.sr, a.length - k0, a.dim);
+        }
+        t = tn;
+    }
+
+    total = group_sum(total);
+    if (q < a.length) {
+        const bool empty = top == -INFINITY && total == 0.f;
+        const float inv = empty ? 0.f : 1.f / total;
+        T* const op = static_cast<T*>(a.o.data) + batch * a.o.sb + head * a.o.sh + q * a.o.sr;
+#pragma unroll
+        for (int dt = 0; dt < S::DT; ++dt) store4<T, UNIT>(op, 16 * dt + 4 * g, a.dim, o[dt] * inv);
+        if (a.lse && g == 0)
+            a.lse[((int64_t)batch * a.heads + head) * a.length + q] = empty ? -INFINITY : top * kLn2 + logf(total);
+    }
+    return true;
+}
+
+template <typename T, int DP, int UNIT, bool CAP>
+__device__ __noinline__ void attend_block_careful(const AttArgs& a, FwdShared<T, DP>& sh, int item)
+{
+    __syncthreads();
+    attend_block<T, DP, UNIT, CAP, true>(a, sh, item);
+}
+
+template <typename T, int DP, int UNIT, bool CAP, int WAVES>
+__global__ __launch_bounds__(kBlock, WAVES) void k_attend(const AttArgs a)
+{
+    __shared__ FwdShared<T, DP> sh;
+    const int item = xcd_item(a.items);
+    if (item < 0) return;
+    if (!attend_block<T, DP, UNIT, CAP, false>(a, sh, item)) attend_block_careful<T, DP, UNIT, CAP>(kernel_args(), sh, item);
+}
+
+}  // namespace
+
+void attend_forward(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s)
+{
+    a.items = a.batch * a.heads * att_blocks(a.length, kTile);
+    by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
+        constexpr int DP = decltype(dp)::value;
+        // blocks per CU that registers allow: accumulators, fragments and the tile under way grow with the row's bytes
+        constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 4 : Shape<decltype(type), DP>::RB <= 256 ? 2 : 2;
+        k_attend<decltype(type), DP, decltype(u)::value, decltype(cap)::value, WAVES><<<att_grid(a.items), dim3(kBlock), 0, s>>>(a);
+    });
+}
+
+}  // namespace gram

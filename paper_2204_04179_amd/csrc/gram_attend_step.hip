@@ -19,7 +19,7 @@ struct StepArgs {
     const int* first;
     const float* table;
     float* part;                      // [batch, heads, splits, dim + 2] when splits > 1
-    int batch, capacity, heads, kv_heads, group, chunks, dim, unit, splits;
+    int batch, capacity, heads, kv_heads, group, chunks, dim, splits;
     float scale, cap;
     AttBuckets bk;
 };
@@ -55,12 +55,14 @@ template <typename T> __device__ __forceinline__ void unpack(u32x4 x, float* v)
     }
 }
 
-template <typename T, int DP, int GC>
+template <typename T, int DP, int UNIT, int GC>
 __global__ __launch_bounds__(kBlock) void k_step(const StepArgs a)
 {
     constexpr int EPC = 16 / sizeof(T), LPK = DP / EPC, KPI = kWave / LPK, U = kStepUnroll;
     __shared__ float s_acc[kWavesPerBlock][GC][DP];
     __shared__ float s_top[kWavesPerBlock][GC], s_total[kWavesPerBlock][GC];
+    __shared__ float s_table[GC][kMaxBorders];
+    __shared__ int s_border[kMaxBorders];
 
     const int split = blockIdx.x % a.splits;
     const int chunk = (blockIdx.x / a.splits) % a.chunks;
@@ -86,31 +88,43 @@ __global__ __launch_bounds__(kBlock) void k_step(const StepArgs a)
     const T* const vn = static_cast<const T*>(a.vn.data) + b * a.vn.sb + kvh * a.vn.sh;
 
     float q[GC][EPC], acc[GC][EPC], top[GC], total[GC], far2[GC];
-    const int last = a.bk.borders ? a.bk.border[a.bk.borders - 1] : a.bk.exact;
+    const RowSource ks = row_source(kn, 0, 1, a.dim), vs = row_source(vn, 0, 1, a.dim);
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
 #pragma unroll
     for (int h = 0; h < GC; ++h) {
         const int head = head0 + (h < heads_here ? h : 0);
-        unpack<T>(load_chunk(static_cast<const T*>(a.q.data) + b * a.q.sb + head * a.q.sh, ch, a.dim, a.unit), q[h]);
+        unpack<T>(load_chunk<T, UNIT>(row_source(static_cast<const T*>(a.q.data) + b * a.q.sb + head * a.q.sh, 0, 1, a.dim), 0u, ch,
+                                      a.dim), q[h]);
         far2[h] = a.bk.side ? a.table[(int64_t)head * buckets + a.bk.side - 1] * kLog2e : 0.f;
+        if ((int)threadIdx.x < buckets) s_table[h][threadIdx.x] = a.table[(int64_t)head * buckets + threadIdx.x] * kLog2e;
         top[h] = -INFINITY, total[h] = 0.f;
 #pragma unroll
         for (int e = 0; e < EPC; ++e) acc[h][e] = 0.f;
     }
     const float z2 = a.scale * kLog2e, zc = a.cap > 0.f ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
 
-    for (int base = lo + wave_id() * (U * KPI); base < hi; base += kWavesPerBlock * U * KPI) {
+    if (threadIdx.x < kMaxBorders) s_border[threadIdx.x] = a.bk.border[threadIdx.x];
+    __syncthreads();
+
+    for (int base = lo + __builtin_amdgcn_readfirstlane(wave_id()) * (U * KPI); base < hi; base += kWavesPerBlock * U * KPI) {
         u32x4 kx[U], vx[U];
         bool in[U];
+        const int held = (hi < n ? hi : n) - base;                   // rows of the round that the cache holds
+        const RowSource kr = row_source(kc + base * a.kc.sr, a.kc.sr, held, a.dim), vr = row_source(vc + base * a.vc.sr, a.vc.sr, held, a.dim);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int row = base + u * KPI + sub;
-            in[u] = row < hi;
-            kx[u] = vx[u] = u32x4{0u, 0u, 0u, 0u};
-            if (in[u]) {
-                kx[u] = load_chunk(row == n ? kn : kc + row * a.kc.sr, ch, a.dim, a.unit);
-                vx[u] = load_chunk(row == n ? vn : vc + row * a.vc.sr, ch, a.dim, a.unit);
-            }
+            const int row = u * KPI + sub;
+            in[u] = base + row < hi;
+            kx[u] = load_chunk<T, UNIT>(kr, row < held ? (uint32_t)row * kr.stride : kNowhere - 256u, ch, a.dim);
+            vx[u] = load_chunk<T, UNIT>(vr, row < held ? (uint32_t)row * vr.stride : kNowhere - 256u, ch, a.dim);
+        }
+        if (base + U * KPI > n) {                                    // the new item, from its own rows
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (base + u * KPI + sub == n) {
+                    kx[u] = load_chunk<T, UNIT>(ks, 0u, ch, a.dim);
+                    vx[u] = load_chunk<T, UNIT>(vs, 0u, ch, a.dim);
+                }
         }
         float s[U][GC];
 #pragma unroll
@@ -127,7 +141,7 @@ __global__ __launch_bounds__(kBlock) void k_step(const StepArgs a)
             }
         }
         if (a.bk.side) {
-            if (n - (base + U * KPI - 1) >= last) {                  // every key of the round in the last bucket
+            if (n - (base + U * KPI - 1) >= a.bk.last) {                  // every key of the round in the last bucket
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -136,10 +150,10 @@ __global__ __launch_bounds__(kBlock) void k_step(const StepArgs a)
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int away = n - (base + u * KPI + sub);
-                    const int bucket = bucket_side(a.bk, away < 0 ? 0 : away);
+                    const int bucket = bucket_side(a.bk, s_border, away < 0 ? 0 : away);
 #pragma unroll
                     for (int h = 0; h < GC; ++h)
-                        s[u][h] += a.table[(int64_t)(head0 + (h < heads_here ? h : 0)) * buckets + bucket] * kLog2e;
+                        s[u][h] += s_table[h][bucket];
                 }
             }
         }
@@ -281,29 +295,22 @@ bool step_launch(const gram_attention_config& c, const AttBuckets& bk, int32_t b
     a.q = q, a.kn = kn, a.vn = vn, a.kc = kc, a.vc = vc, a.o = o;
     a.lengths = lengths, a.first = first, a.table = table, a.part = static_cast<float*>(work);
     a.batch = batch, a.capacity = capacity, a.heads = c.heads, a.kv_heads = c.kv_heads, a.group = c.heads / c.kv_heads;
-    a.dim = c.head_dim, a.unit = unit, a.scale = c.scale, a.cap = c.cap, a.bk = bk;
+    a.dim = c.head_dim, a.scale = c.scale, a.cap = c.cap, a.bk = bk;
     const int gc = step_heads(a.group);
     a.chunks = (a.group + gc - 1) / gc;
     a.splits = step_splits(c, batch, capacity);
     const int64_t blocks = (int64_t)batch * c.kv_heads * a.chunks * a.splits;
     if (blocks > kAttMaxBlocks || (int64_t)batch * c.heads > kAttMaxBlocks) return false;
-    auto go = [&](auto type, auto dp) {
+    by_shape(c, unit, [&](auto type, auto dp, auto u) {
         using T = decltype(type);
-        constexpr int DP = decltype(dp)::value;
+        constexpr int DP = decltype(dp)::value, UNIT = decltype(u)::value;
         const dim3 grid((unsigned)blocks);
-        if (gc == 1) k_step<T, DP, 1><<<grid, dim3(kBlock), 0, s>>>(a);
-        else if (gc == 2) k_step<T, DP, 2><<<grid, dim3(kBlock), 0, s>>>(a);
-        else if (gc == 4) k_step<T, DP, 4><<<grid, dim3(kBlock), 0, s>>>(a);
-        else k_step<T, DP, 8><<<grid, dim3(kBlock), 0, s>>>(a);
+        if (gc == 1) k_step<T, DP, UNIT, 1><<<grid, dim3(kBlock), 0, s>>>(a);
+        else if (gc == 2) k_step<T, DP, UNIT, 2><<<grid, dim3(kBlock), 0, s>>>(a);
+        else if (gc == 4) k_step<T, DP, UNIT, 4><<<grid, dim3(kBlock), 0, s>>>(a);
+        else k_step<T, DP, UNIT, 8><<<grid, dim3(kBlock), 0, s>>>(a);
         if (a.splits > 1) k_step_join<T><<<dim3((unsigned)(batch * c.heads)), dim3(128), 0, s>>>(a);
-    };
-    auto width = [&](auto type) {
-        if (c.head_dim <= 32) go(type, std::integral_constant<int, 32>{});
-        else if (c.head_dim <= 64) go(type, std::integral_constant<int, 64>{});
-        else go(type, std::integral_constant<int, 128>{});
-    };
-    if (c.dtype == GRAM_BF16) width(Bf16{});
-    else width(float{});
+    });
     return true;
 }
 
