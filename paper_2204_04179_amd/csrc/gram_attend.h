@@ -63,11 +63,21 @@ struct AttArgs {
     AttBuckets bk;
 };
 
-// The kernel's argument block where it lies in memory, to hand to a function that is called: the address of the parameter
-// itself would make every lane keep a copy of it.  For kernels whose one parameter is an AttArgs.
-__device__ __forceinline__ const AttArgs& kernel_args()
+// For kernels whose one parameter is an AttArgs: its borders where the arguments lie in memory (a lane's own index into the
+// parameter would make a copy of it), and the arguments read once more, so that none of them is held in a register
+// through the first form of a block for the sake of a second one that hardly ever runs.
+typedef const __attribute__((address_space(4))) AttArgs* KernelArgs;
+__device__ __forceinline__ const int* kernel_borders()
 {
-    return *(const AttArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    return (const int*)((const char*)__builtin_amdgcn_kernarg_segment_ptr() + __builtin_offsetof(AttArgs, bk.border));
+}
+__device__ __forceinline__ AttArgs args_again()
+{
+    uint64_t at = (uint64_t)(uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    AttArgs a;
+    __builtin_memcpy(&a, (KernelArgs)at, sizeof a);
+    return a;
 }
 
 // By value: a bit cast applied to an element of a vector yields the vector's first element.
@@ -158,27 +168,6 @@ template <typename T, int UNIT> __device__ __forceinline__ void store4(T* __rest
 }
 
 __device__ __forceinline__ bool nonfinite_bits(uint32_t f32_bits) { return (f32_bits & 0x7f800000u) == 0x7f800000u; }
-
-// Collects what has_nonfinite needs of a chunk: the largest exponent seen, for each 16-bit half (bf16) or word.
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-template <typename T> __device__ __forceinline__ uint32_t max_exponent(uint32_t most, u32x4 v)
-{
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if constexpr (sizeof(T) == 2) {
-            const uint32_t x = v[e] & 0x7f807f80u;
-            most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most), __builtin_bit_cast(u16x2, x)));
-        } else {
-            const uint32_t x = v[e] & 0x7f800000u;
-            most = most > x ? most : x;
-        }
-    }
-    return most;
-}
-template <typename T> __device__ __forceinline__ bool has_nonfinite(uint32_t most)
-{
-    return (most & 0x7f800000u) == 0x7f800000u || (sizeof(T) == 2 && (most & 0x7f80u) == 0x7f80u);
-}
 
 // Replaces non-finite elements of a chunk by zero; true if there was one.
 template <typename T> __device__ __forceinline__ bool clean_chunk(u32x4& v)
@@ -330,12 +319,14 @@ __device__ __forceinline__ void add_nonfinite(f32x4 (&acc)[DP / 16], const f32x4
             const float wk = __shfl(wi, g2 * 16 + c);
             const int vk = __shfl(vi, g2 * 16 + c);
             if (row >= rows) continue;
+            int cols = dim - 4 * g;
+            asm volatile("" : "+v"(cols));       // or 4 DT comparisons are held in registers through the loops
 #pragma unroll
             for (int dt = 0; dt < Shape<T, DP>::DT; ++dt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int col = 16 * dt + 4 * g + e;
-                    if (col < dim && vk) {
+                    if (16 * dt + e < cols && vk) {
                         const float x = load_elem(base + row * sr + col);
                         if (nonfinite_bits(__builtin_bit_cast(uint32_t, x))) acc[dt][e] += wk * x;
                     }
@@ -460,6 +451,13 @@ __device__ __forceinline__ int uniform_bucket(const AttBuckets& bk, int lo, int 
     return -1;
 }
 
+// ---- non-finite values ------------------------------------------------------------------------------------
+//
+// A masked pair has weight zero, and zero times an infinity or a NaN of the streamed tile is not zero: a second product would
+// carry such a value to owner rows that do not see it.  A block therefore runs in its common form, which does not care, and
+// looks at its accumulators before it writes: if none holds a non-finite value, no product met one.  Otherwise it starts
+// again in its careful form, which gives the value to the rows that see it and to no others.
+
 // ---- walking the streamed rows ----------------------------------------------------------------------------
 
 // Work item of a block: the blocks of one head of one history share its rows, so neighbours in this order go to one XCD
@@ -553,10 +551,10 @@ template <typename T, int DP, int UNIT> struct Feed {
         }
         seg = row_segment(segments, row0 + lane_id(), length);
     }
-    // guard: pairs of the tile are masked, so a non-finite element would reach rows that do not see it.  CAREFUL: they are
-    // replaced by zeros in the operands named (those that enter a second product) and flagged; else only flagged.
+    // CAREFUL, of a tile with masked pairs: non-finite elements of the operands named (those that enter a second product) are
+    // replaced by zeros, and flags[wave] says whether there were any.
     template <bool CAREFUL, bool A, bool B>
-    __device__ __forceinline__ void put(unsigned char* ta, unsigned char* tb, int* s_seg, bool guard, bool odd, uint32_t* flags)
+    __device__ __forceinline__ void put(unsigned char* ta, unsigned char* tb, int* s_seg, bool masked, uint32_t* flags)
     {
         const int row = threadIdx.x / S::NCH, ch = threadIdx.x % S::NCH;
         const uint64_t there = __ballot(seg != kNoSeg);
@@ -565,23 +563,17 @@ template <typename T, int DP, int UNIT> struct Feed {
             for (int i = 0; i < S::NC; ++i)
                 if (!((there >> (row + i * STEP)) & 1)) a[i] = b[i] = u32x4{0u, 0u, 0u, 0u};
         }
-        if (guard) {
-            if constexpr (CAREFUL) {
+        if constexpr (CAREFUL) {
+            bool odd = false;
+            if (masked) {
 #pragma unroll
                 for (int i = 0; i < S::NC; ++i) {
                     if (A) odd |= clean_chunk<T>(a[i]);
                     if (B) odd |= clean_chunk<T>(b[i]);
                 }
-            } else {
-                uint32_t most = 0u;
-#pragma unroll
-                for (int i = 0; i < S::NC; ++i) most = max_exponent<T>(max_exponent<T>(most, a[i]), b[i]);
-                odd |= has_nonfinite<T>(most);
             }
             odd = __any(odd);
             if (lane_id() == 0) flags[wave_id()] = odd;
-        } else if (CAREFUL && lane_id() == 0) {
-            flags[wave_id()] = 0u;
         }
         if (wave_id() == 0) s_seg[lane_id()] = seg;
 #pragma unroll
@@ -647,6 +639,21 @@ __device__ __forceinline__ void load_owner(u32x4 (&f)[DP * sizeof(T) / 64], cons
         f[kk] = load_chunk<T, UNIT>(src, (uint32_t)c * src.stride, g + 4 * kk, dim);
         if (!live) f[kk] = u32x4{0u, 0u, 0u, 0u};
     }
+}
+
+// Whether a non-finite value is among a wave's accumulators.
+template <int N> __device__ __forceinline__ bool any_nonfinite(const f32x4 (&acc)[N])
+{
+    uint32_t most = 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float v = acc[i][r];
+            const uint32_t e = __builtin_bit_cast(uint32_t, v) & 0x7f800000u;
+            most = most > e ? most : e;
+        }
+    return nonfinite_bits(most);
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------

@@ -9,18 +9,21 @@ namespace gram {
 namespace {
 
 // dtable[head, b] = the sum of the blocks' partial rows, strand by strand in a fixed order.
-__global__ __launch_bounds__(kBlock) void k_attend_dtable(const float* __restrict__ part, int parts, int buckets,
-                                                          float* __restrict__ dtable)
+__global__ __launch_bounds__(1024) void k_attend_dtable(const float* __restrict__ part, int parts, int buckets,
+                                                        float* __restrict__ dtable)
 {
-    __shared__ double s[kBlock];
+    __shared__ double s[1024];
     const int head = blockIdx.y, b = blockIdx.x * 16 + threadIdx.x % 16, strand = threadIdx.x / 16;
     double sum = 0.0;
-    if (b < buckets)
-        for (int p = strand; p < parts; p += 16) sum += (double)part[((int64_t)head * parts + p) * buckets + b];
+    if (b < buckets) {
+        const float* const p = part + (int64_t)head * parts * buckets + b;
+#pragma unroll 8
+        for (int i = strand; i < parts; i += 64) sum += (double)p[(int64_t)i * buckets];
+    }
     s[threadIdx.x] = sum;
     __syncthreads();
     if (strand == 0 && b < buckets) {
-        for (int k = 1; k < 16; ++k) sum += s[k * 16 + threadIdx.x];
+        for (int k = 1; k < 64; ++k) sum += s[k * 16 + threadIdx.x];
         dtable[(int64_t)head * buckets + b] = (float)sum;
     }
 }
@@ -205,7 +208,7 @@ int gram_attention_backward(const gram_attention_config* cfg, int32_t batch, int
         attend_backward_keys(*cfg, a, unit, s);
     }
     if (dtable)
-        k_attend_dtable<<<dim3((unsigned)((cfg->buckets + 15) / 16), (unsigned)cfg->heads), dim3(kBlock), 0, s>>>(
+        k_attend_dtable<<<dim3((unsigned)((cfg->buckets + 15) / 16), (unsigned)cfg->heads), dim3(1024), 0, s>>>(
             a.part, none ? 0 : a.parts, cfg->buckets, dtable);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? GRAM_OK : fail_call(GRAM_ERR_HIP, "gram_attention_backward: %s", hipGetErrorString(e));

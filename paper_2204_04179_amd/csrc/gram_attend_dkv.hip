@@ -23,11 +23,12 @@ template <typename T, int DP, int UNIT, bool CAP, bool CAREFUL>
 __device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh, int item)
 {
     using S = Shape<T, DP>;
+    constexpr bool AHEAD = !CAREFUL && S::RB < 256;
     const int ntiles = (a.length + kTile - 1) / kTile;
     const int kt = item % ntiles;
     const int kvh = (item / ntiles) % a.kv_heads, batch = item / ntiles / a.kv_heads;
-    const int c = lane_id() & 15, g = lane_id() >> 4;
-    const int k0 = kt * kTile, wk0 = k0 + wave_id() * 16, k = wk0 + c;
+    const int c = lane_id() & 15, g = lane_id() >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int k0 = kt * kTile, wk0 = k0 + wave * 16, k = wk0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
     const int prefix = a.prefix ? a.prefix[batch] : 0;
 
@@ -41,7 +42,7 @@ __device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh
     const int own = live ? kseg : kNoSegOwner;
     const int t0 = a.causal && k0 >= prefix ? kt : 0;
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
-    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = a.bk.border[threadIdx.x];
+    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = kernel_borders()[threadIdx.x];
     if (seg) mark_tiles(sh.marks, seg, a.length, kseg, k < a.length, t0, ntiles);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;
 
@@ -54,6 +55,7 @@ __device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh
     const float z2 = a.scale * kLog2e, zc = CAP ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
     const int first = a.causal && k >= prefix ? k : 0;            // queries from it on see the key, segments aside
 
+    const bool causal_bias = a.causal && prefix <= 0;             // as in the pass over the queries
     // whether all pairs of the query tile with keys up to `row` are visible
     auto whole = [&](int t, int row, bool mixed) {
         const int q0 = t * kTile;
@@ -70,27 +72,24 @@ __device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh
     };
 
     int h = 0, t = next_tile(t0, ntiles, mk);
-    if (t < ntiles) load(0, t);
+    if (AHEAD && t < ntiles) load(0, t);
     while (t < ntiles) {
+        if (!AHEAD) load(h, t);
         const bool mixed = tile_mixed(mk, t);
-        const bool guard = !whole(t, k0 + kTile - 1, mixed);
         const int q0 = t * kTile, lo = q0 - (k0 + kTile - 1);     // the smallest distance of the block's pairs
         const int flat = a.bk.side ? uniform_bucket(a.bk, lo, lo + 2 * kTile - 2) : 0;
         const float* const table = a.table + (int64_t)(kvh * a.group + h) * buckets;
         const float lse2 = row_lse == -INFINITY ? 0.f : row_lse * kLog2e;
-        // a query whose statistics are not finite would reach keys that it does not see
-        const bool odd_row = nonfinite_bits(__builtin_bit_cast(uint32_t, lse2)) || nonfinite_bits(__builtin_bit_cast(uint32_t, row_delta));
         __syncthreads();
-        feed.template put<CAREFUL, true, true>(sh.q, sh.d, sh.seg, guard, odd_row, sh.flags);
+        feed.template put<CAREFUL, true, true>(sh.q, sh.d, sh.seg, CAREFUL && !whole(t, k0 + kTile - 1, mixed), sh.flags);
         if (wave_id() == 0) sh.lse[lane_id()] = lse2, sh.delta[lane_id()] = feed.seg == kNoSeg ? 0.f : row_delta;
         if (flat < 0 && (int)threadIdx.x < 2 * kTile - 1)
-            sh.bias[threadIdx.x] = table[bucket_of(a.bk, sh.border, lo + (int)threadIdx.x)] * kLog2e;
+            sh.bias[threadIdx.x] = causal_bias && lo + (int)threadIdx.x < 0 ? -INFINITY : table[bucket_of(a.bk, sh.border, lo + (int)threadIdx.x)] * kLog2e;
         int hn = h, tn = next_tile(t + 1, ntiles, mk);
         if (tn >= ntiles && h + 1 < a.group) hn = h + 1, tn = next_tile(t0, ntiles, mk);
-        if (tn < ntiles) load(hn, tn);
+        if (AHEAD && tn < ntiles) load(hn, tn);
         __syncthreads();
-        const bool odd = (CAREFUL || guard) && any_flag(sh.flags);
-        if (!CAREFUL && odd) return false;
+        const bool odd = CAREFUL && any_flag(sh.flags);
         if (wk0 < a.length && !(a.causal && q0 + kTile - 1 < wk0 && wk0 >= prefix)) {
             f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
             first_product<T, DP>(s, kf, rd, sh.q);
@@ -104,7 +103,7 @@ __device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh
                     for (int r = 0; r < 4; ++r) s[n][r] += bias[16 * n + r];
             }
             uint32_t vis = 0xffffu;
-            if (!whole(t, wk0 + 15, mixed)) {
+            if (!whole(t, wk0 + 15, mixed) && !(causal_bias && flat < 0 && !mixed)) {
                 if (CAREFUL) vis = visible_bits<true>(sh.seg, own, first - q0, kTile);
                 if (mixed) mask_scores<true, true>(s, sh.seg, own, first - q0);
                 else mask_scores<false, true>(s, sh.seg, own, first - q0);
@@ -138,6 +137,7 @@ __device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh
         h = hn, t = tn;
     }
 
+    if (!CAREFUL && __syncthreads_or(any_nonfinite(dk) || any_nonfinite(dv))) return false;
     if (k < a.length) {
         T* const dkp = static_cast<T*>(a.dk.data) + batch * a.dk.sb + kvh * a.dk.sh + k * a.dk.sr;
         T* const dvp = static_cast<T*>(a.dv.data) + batch * a.dv.sb + kvh * a.dv.sh + k * a.dv.sr;
@@ -150,20 +150,15 @@ __device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh
     return true;
 }
 
-template <typename T, int DP, int UNIT, bool CAP>
-__device__ __noinline__ void dkv_block_careful(const AttArgs& a, DkvShared<T, DP>& sh, int item)
-{
-    __syncthreads();
-    dkv_block<T, DP, UNIT, CAP, true>(a, sh, item);
-}
-
 template <typename T, int DP, int UNIT, bool CAP, int WAVES>
 __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dkv(const AttArgs a)
 {
     __shared__ DkvShared<T, DP> sh;
     const int item = xcd_item(a.items);
     if (item < 0) return;
-    if (!dkv_block<T, DP, UNIT, CAP, false>(a, sh, item)) dkv_block_careful<T, DP, UNIT, CAP>(kernel_args(), sh, item);
+    if (dkv_block<T, DP, UNIT, CAP, false>(a, sh, item)) return;
+    __syncthreads();
+    dkv_block<T, DP, UNIT, CAP, true>(args_again(), sh, item);
 }
 
 }  // namespace
@@ -173,7 +168,7 @@ void attend_backward_keys(const gram_attention_config& c, AttArgs a, int unit, h
     a.items = a.batch * a.kv_heads * att_blocks(a.length, kTile);
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
-        constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 3 : 2;
+        constexpr int WAVES = Shape<decltype(type), DP>::RB <= 256 ? 3 : 2;
         k_attend_dkv<decltype(type), DP, decltype(u)::value, decltype(cap)::value, WAVES><<<att_grid(a.items), dim3(kBlock), 0, s>>>(a);
     });
 }

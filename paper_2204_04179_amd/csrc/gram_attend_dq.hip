@@ -94,11 +94,12 @@ template <typename T, int DP, int UNIT, bool CAP, bool CAREFUL>
 __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, float* dist, int item)
 {
     using S = Shape<T, DP>;
+    constexpr bool AHEAD = !CAREFUL && S::RB < 256;
     const int nqt = (a.length + kTile - 1) / kTile;
     const int qt = nqt - 1 - item % nqt;
     const int head = (item / nqt) % a.heads, batch = item / nqt / a.heads, kvh = head / a.group;
-    const int c = lane_id() & 15, g = lane_id() >> 4;
-    const int q0 = qt * kTile, wq0 = q0 + wave_id() * 16, q = wq0 + c;
+    const int c = lane_id() & 15, g = lane_id() >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int q0 = qt * kTile, wq0 = q0 + wave * 16, q = wq0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
     const int prefix = a.prefix ? a.prefix[batch] : 0;
     const T* const kp = static_cast<const T*>(a.k.data) + batch * a.k.sb + kvh * a.k.sh;
@@ -135,7 +136,7 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
     }
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
     if ((int)threadIdx.x < buckets) sh.table[threadIdx.x] = a.table[(int64_t)head * buckets + threadIdx.x] * kLog2e;
-    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = a.bk.border[threadIdx.x];
+    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = kernel_borders()[threadIdx.x];
     if (want_table) {
         for (int i = threadIdx.x; i < kWavesPerBlock * (2 * kNear + 1); i += kBlock) dist[i] = 0.f;
         for (int i = threadIdx.x; i < kWavesPerBlock * 4 * kStrip; i += kBlock) (&sh.strip[0][0][0])[i] = 0.f;
@@ -162,6 +163,7 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
     int flat_bucket = -1;
     float flat_sum = 0.f;
 
+    const bool causal_bias = a.causal && prefix <= 0;             // as in the forward pass
     auto whole = [&](int t, int row, bool mixed) {
         const int k1 = t * kTile + kTile;
         return !mixed && k1 <= a.length && (!a.causal || k1 - 1 <= row || k1 <= prefix);
@@ -174,25 +176,24 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
     // DELTA: only sum p dp; else the gradients, with that sum on the way where the one tile holds it all
     const int tfirst = next_tile(0, t1, mk);
     const bool one_tile = want_table && next_tile(tfirst + 1, t1, mk) >= t1;
-    auto walk = [&](auto delta_only) -> bool {
+    auto walk = [&](auto delta_only) {
         constexpr bool DELTA = decltype(delta_only)::value;
         int t = tfirst;
-        if (t < t1) load(t);
+        if (AHEAD && t < t1) load(t);
         while (t < t1) {
             const bool mixed = tile_mixed(mk, t);
-            const bool guard = !whole(t, q0, mixed);
             const int k0 = t * kTile, hi = q0 + kTile - 1 - k0;
             const int flat = a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
+            if (!AHEAD) load(t);
             __syncthreads();
-            feed.template put<CAREFUL, true, false>(sh.k, sh.v, sh.seg, guard, false, sh.flags);
+            feed.template put<CAREFUL, true, false>(sh.k, sh.v, sh.seg, CAREFUL && !whole(t, q0, mixed), sh.flags);
             if (flat < 0 && (int)threadIdx.x < 2 * kTile - 1) {
-                sh.bias[threadIdx.x] = sh.table[bucket_of(a.bk, sh.border, hi - (int)threadIdx.x)];
+                sh.bias[threadIdx.x] = causal_bias && hi < (int)threadIdx.x ? -INFINITY : sh.table[bucket_of(a.bk, sh.border, hi - (int)threadIdx.x)];
             }
             const int tn = next_tile(t + 1, t1, mk);
-            if (tn < t1) load(tn);
+            if (AHEAD && tn < t1) load(tn);
             __syncthreads();
-            const bool odd = (CAREFUL || guard) && any_flag(sh.flags);
-            if (!CAREFUL && odd) return false;
+            const bool odd = CAREFUL && any_flag(sh.flags);
             if (wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix)) {
                 f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
                 first_product<T, DP>(s, qf, rd, sh.k);
@@ -206,7 +207,7 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
                         for (int r = 0; r < 4; ++r) s[n][r] += bias[16 * n + r];
                 }
                 uint32_t vis = 0xffffu;
-                if (!whole(t, wq0, mixed) || !full_rows) {
+                if ((!whole(t, wq0, mixed) && !(causal_bias && flat < 0 && !mixed)) || !full_rows) {
                     if (CAREFUL && odd) vis = visible_bits<true>(sh.seg, own, 0, last - k0);
                     if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0);
                     else mask_scores<false, false>(s, sh.seg, own, last - k0);
@@ -255,10 +256,10 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
             t = tn;
         }
         if constexpr (DELTA) delta = group_sum(delta);
-        return true;
     };
-    if (want_table && !one_tile && !walk(std::true_type{})) return false;
-    if (!walk(std::false_type{})) return false;
+    if (want_table && !one_tile) walk(std::true_type{});
+    walk(std::false_type{});
+    if (!CAREFUL && __syncthreads_or(any_nonfinite(dq))) return false;
 
     if (q < a.length) {
         T* const dqp = static_cast<T*>(a.dq.data) + batch * a.dq.sb + head * a.dq.sh + q * a.dq.sr;
@@ -294,13 +295,6 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
     return true;
 }
 
-template <typename T, int DP, int UNIT, bool CAP>
-__device__ __noinline__ void dq_block_careful(const AttArgs& a, DqShared<T, DP>& sh, float* dist, int item)
-{
-    __syncthreads();
-    dq_block<T, DP, UNIT, CAP, true>(a, sh, dist, item);
-}
-
 template <typename T, int DP, int UNIT, bool CAP, int WAVES>
 __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
 {
@@ -308,7 +302,9 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
     __shared__ DqShared<T, DP> sh;
     const int item = xcd_item(a.items);
     if (item < 0) return;
-    if (!dq_block<T, DP, UNIT, CAP, false>(a, sh, s_dist, item)) dq_block_careful<T, DP, UNIT, CAP>(kernel_args(), sh, s_dist, item);
+    if (dq_block<T, DP, UNIT, CAP, false>(a, sh, s_dist, item)) return;
+    __syncthreads();
+    dq_block<T, DP, UNIT, CAP, true>(args_again(), sh, s_dist, item);
 }
 
 }  // namespace

@@ -21,18 +21,18 @@ template <typename T, int DP> struct FwdShared {
     TileMarks marks;
 };
 
-// One block: 64 queries of one head, 16 to a wave.  False (CAREFUL not set): a tile with masked pairs holds a non-finite
-// element, nothing has been written, and the block starts again with the careful form.  Apart, so that the registers of the
-// rare form are not the common one's.
+// One block: 64 queries of one head, 16 to a wave.  False (CAREFUL not set): an accumulator is not finite and nothing has
+// been written.
 template <typename T, int DP, int UNIT, bool CAP, bool CAREFUL>
 __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>& sh, int item)
 {
     using S = Shape<T, DP>;
+    constexpr bool AHEAD = !CAREFUL && S::RB < 256;
     const int nqt = (a.length + kTile - 1) / kTile;
     const int qt = nqt - 1 - item % nqt;                 // the longest rows of a causal mask first
     const int head = (item / nqt) % a.heads, batch = item / nqt / a.heads, kvh = head / a.group;
-    const int c = lane_id() & 15, g = lane_id() >> 4;
-    const int q0 = qt * kTile, wq0 = q0 + wave_id() * 16, q = wq0 + c;
+    const int c = lane_id() & 15, g = lane_id() >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int q0 = qt * kTile, wq0 = q0 + wave * 16, q = wq0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
     const int prefix = a.prefix ? a.prefix[batch] : 0;
     const T* const kp = static_cast<const T*>(a.k.data) + batch * a.k.sb + kvh * a.k.sh;
@@ -53,7 +53,7 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
     }
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
     if ((int)threadIdx.x < buckets) sh.table[threadIdx.x] = a.table[(int64_t)head * buckets + threadIdx.x] * kLog2e;
-    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = a.bk.border[threadIdx.x];
+    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = kernel_borders()[threadIdx.x];
     if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;
 
@@ -70,6 +70,8 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
         last = last < a.length ? last : a.length;
     }
 
+    // causal, no prefix: the bias is minus infinity at negative distances, and tiles of one segment need no other mask
+    const bool causal_bias = a.causal && prefix <= 0;
     // whether all pairs of the tile with rows from `row` on are visible
     auto whole = [&](int t, int row, bool mixed) {
         const int k1 = t * kTile + kTile;
@@ -81,21 +83,20 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
     };
 
     int t = next_tile(0, t1, mk);
-    if (t < t1) load(t);
+    if (AHEAD && t < t1) load(t);
     while (t < t1) {
         const bool mixed = tile_mixed(mk, t);
-        const bool guard = !whole(t, q0, mixed);
         const int k0 = t * kTile, hi = q0 + kTile - 1 - k0;       // the largest distance of the block's pairs
         const int flat = a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
+        if (!AHEAD) load(t);
         __syncthreads();                                          // the tile before has been read
-        feed.template put<CAREFUL, false, true>(sh.k, sh.v, sh.seg, guard, false, sh.flags);
+        feed.template put<CAREFUL, false, true>(sh.k, sh.v, sh.seg, CAREFUL && !whole(t, q0, mixed), sh.flags);
         if (flat < 0 && (int)threadIdx.x < 2 * kTile - 1)
-            sh.bias[threadIdx.x] = sh.table[bucket_of(a.bk, sh.border, hi - (int)threadIdx.x)];
+            sh.bias[threadIdx.x] = causal_bias && hi < (int)threadIdx.x ? -INFINITY : sh.table[bucket_of(a.bk, sh.border, hi - (int)threadIdx.x)];
         const int tn = next_tile(t + 1, t1, mk);
-        if (tn < t1) load(tn);
+        if (AHEAD && tn < t1) load(tn);
         __syncthreads();
-        const bool odd = (CAREFUL || guard) && any_flag(sh.flags);
-        if (!CAREFUL && odd) return false;
+        const bool odd = CAREFUL && any_flag(sh.flags);
         if (wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix)) {
             f32x4 s[4], slope[CAP ? 4 : 1];
             first_product<T, DP>(s, qf, rd, sh.k);
@@ -109,7 +110,7 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
                     for (int r = 0; r < 4; ++r) s[n][r] += bias[16 * n + r];
             }
             uint32_t vis = 0xffffu;
-            if (!whole(t, wq0, mixed)) {
+            if (!whole(t, wq0, mixed) && !(causal_bias && flat < 0 && !mixed)) {
                 if (CAREFUL && odd) vis = visible_bits<true>(sh.seg, own, 0, last - k0);
                 if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0);
                 else mask_scores<false, false>(s, sh.seg, own, last - k0);
@@ -141,6 +142,7 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
     }
 
     total = group_sum(total);
+    if (!CAREFUL && __syncthreads_or(any_nonfinite(o))) return false;
     if (q < a.length) {
         const bool empty = top == -INFINITY && total == 0.f;
         const float inv = empty ? 0.f : 1.f / total;
@@ -153,20 +155,15 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
     return true;
 }
 
-template <typename T, int DP, int UNIT, bool CAP>
-__device__ __noinline__ void attend_block_careful(const AttArgs& a, FwdShared<T, DP>& sh, int item)
-{
-    __syncthreads();
-    attend_block<T, DP, UNIT, CAP, true>(a, sh, item);
-}
-
 template <typename T, int DP, int UNIT, bool CAP, int WAVES>
 __global__ __launch_bounds__(kBlock, WAVES) void k_attend(const AttArgs a)
 {
     __shared__ FwdShared<T, DP> sh;
     const int item = xcd_item(a.items);
     if (item < 0) return;
-    if (!attend_block<T, DP, UNIT, CAP, false>(a, sh, item)) attend_block_careful<T, DP, UNIT, CAP>(kernel_args(), sh, item);
+    if (attend_block<T, DP, UNIT, CAP, false>(a, sh, item)) return;
+    __syncthreads();
+    attend_block<T, DP, UNIT, CAP, true>(args_again(), sh, item);
 }
 
 }  // namespace
@@ -177,7 +174,7 @@ void attend_forward(const gram_attention_config& c, AttArgs a, int unit, hipStre
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
         // blocks per CU that registers allow: accumulators, fragments and the tile under way grow with the row's bytes
-        constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 4 : Shape<decltype(type), DP>::RB <= 256 ? 2 : 2;
+        constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 4 : Shape<decltype(type), DP>::RB <= 256 ? 3 : 2;
         k_attend<decltype(type), DP, decltype(u)::value, decltype(cap)::value, WAVES><<<att_grid(a.items), dim3(kBlock), 0, s>>>(a);
     });
 }
