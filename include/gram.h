@@ -469,8 +469,9 @@ int32_t gram_distance_bucket(const gram_attention_config* cfg, int32_t distance)
  *   table    DEVICE [heads, buckets] float32 (NULL if buckets is 0)
  *   lse      DEVICE [batch, heads, length] float32, nullable  out: log sum_j exp s_ij
  *            for the backward pass (-inf for a query that sees nothing)
- * A NaN or infinity at a position reaches the outputs of the queries that see it
- * and no others. */
+ * A NaN or infinity in a key or value makes the rows of the queries that see it
+ * non-finite (where it lies among pairs that are masked the whole row is NaN) and
+ * reaches no other row; so it is with every operand of the backward pass. */
 int gram_attention(const gram_attention_config* cfg, int32_t batch, int32_t length, const gram_rows* q,
                    const gram_rows* k, const gram_rows* v, const gram_rows* o, const int32_t* segments,
                    const int32_t* prefix, const float* table, float* lse, void* stream);

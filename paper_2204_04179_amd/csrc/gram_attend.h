@@ -64,20 +64,10 @@ struct AttArgs {
 };
 
 // For kernels whose one parameter is an AttArgs: its borders where the arguments lie in memory (a lane's own index into the
-// parameter would make a copy of it), and the arguments read once more, so that none of them is held in a register
-// through the first form of a block for the sake of a second one that hardly ever runs.
-typedef const __attribute__((address_space(4))) AttArgs* KernelArgs;
+// parameter would make a copy of it).
 __device__ __forceinline__ const int* kernel_borders()
 {
     return (const int*)((const char*)__builtin_amdgcn_kernarg_segment_ptr() + __builtin_offsetof(AttArgs, bk.border));
-}
-__device__ __forceinline__ AttArgs args_again()
-{
-    uint64_t at = (uint64_t)(uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
-    asm volatile("" : "+s"(at));
-    AttArgs a;
-    __builtin_memcpy(&a, (KernelArgs)at, sizeof a);
-    return a;
 }
 
 // By value: a bit cast applied to an element of a vector yields the vector's first element.
@@ -93,10 +83,16 @@ template <typename T, int DP> struct Shape {
     static constexpr int TILE = kTile * RB;
 };
 
-// 16-byte chunk `ch` of row `row` lies at chunk ch ^ swz(row): the 16 rows of a fragment read start in different banks.
-template <int NCH> __device__ __forceinline__ int swz(int row)
+// 16-byte chunk `ch` of row `row` lies at chunk ch ^ swz(row), so that no read of a tile meets a bank twice: 64 banks hold
+// one row of 16 chunks, two of 8, four of 4.  A fragment along rows takes the same chunk of 16 rows, eight lanes at a time.  A
+// transposed one of bf16 takes two neighbouring chunks of four neighbouring rows (hence the shift by one chunk), of float32
+// four neighbouring chunks of rows 4 apart.
+template <typename T, int NCH> __device__ __forceinline__ int swz(int row)
 {
-    return NCH >= 16 ? row & 15 : NCH == 8 ? row & 7 : (row >> 1) & 3;
+    if constexpr (sizeof(T) == 2)
+        return NCH >= 16 ? ((row & 7) << 1) | ((row >> 3) & 1) : NCH == 8 ? (row & 6) | ((row >> 3) & 1) : (row >> 2) & 3;
+    else
+        return NCH >= 16 ? row & 15 : row & 7;
 }
 
 // ---- global rows ------------------------------------------------------------------------------------------
@@ -145,51 +141,7 @@ template <typename T, int UNIT> __device__ __forceinline__ u32x4 load_chunk(cons
     }
 }
 
-// Four neighbouring elements at column `at`.
-template <typename T, int UNIT> __device__ __forceinline__ void store4(T* __restrict__ row, int at, int dim, f32x4 v)
-{
-    if constexpr (UNIT >= 8) {       // rows are whole groups of four elements
-        if (at < dim) {
-            if constexpr (sizeof(T) == 2) {
-                const u32x2 t = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                *reinterpret_cast<u32x2*>(row + at) = t;
-            } else {
-                *reinterpret_cast<f32x4*>(row + at) = v;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (at + e < dim) {
-                if constexpr (sizeof(T) == 2) row[at + e].bits = (uint16_t)pack_bf16x2(v[e], 0.f);
-                else row[at + e] = v[e];
-            }
-    }
-}
-
 __device__ __forceinline__ bool nonfinite_bits(uint32_t f32_bits) { return (f32_bits & 0x7f800000u) == 0x7f800000u; }
-
-// Replaces non-finite elements of a chunk by zero; true if there was one.
-template <typename T> __device__ __forceinline__ bool clean_chunk(u32x4& v)
-{
-    bool any = false;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if constexpr (sizeof(T) == 2) {
-            if ((v[e] & 0x7f80u) == 0x7f80u) any = true, v[e] &= 0xffff0000u;
-            if (nonfinite_bits(v[e])) any = true, v[e] &= 0x0000ffffu;
-        } else {
-            if (nonfinite_bits(v[e])) any = true, v[e] = 0u;
-        }
-    }
-    return any;
-}
-
-template <typename T> __device__ __forceinline__ float load_elem(const T* p)
-{
-    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(float, (uint32_t)p->bits << 16);
-    else return *p;
-}
 
 // ---- fragments --------------------------------------------------------------------------------------------
 
@@ -213,20 +165,20 @@ template <typename T, int DP> struct Reader {
     int direct[S::KK];       // rows c of a block, chunk g + 4 kk
     int trans[S::DT];        // bf16: the transposing read's piece; float32: row 4 g of a block, column 16 dt + c
 
-    __device__ __forceinline__ Reader()
+    __device__ __forceinline__ explicit Reader(int lane)
     {
-        const int c = lane_id() & 15, g = lane_id() >> 4;
+        const int c = lane & 15, g = lane >> 4;
 #pragma unroll
-        for (int kk = 0; kk < S::KK; ++kk) direct[kk] = c * S::RB + (((g + 4 * kk) ^ swz<S::NCH>(c)) * 16);
+        for (int kk = 0; kk < S::KK; ++kk) direct[kk] = c * S::RB + (((g + 4 * kk) ^ swz<T, S::NCH>(c)) * 16);
 #pragma unroll
         for (int dt = 0; dt < S::DT; ++dt) {
             if constexpr (sizeof(T) == 2) {
                 // group g reads rows 4 g .. 4 g + 3 of a block: lane j of it supplies row j / 4, columns 4 (j % 4) .. + 3
                 // and receives column j of the four rows
                 const int row = 4 * g + (c >> 2);
-                trans[dt] = row * S::RB + (((2 * dt + ((c & 3) >> 1)) ^ swz<S::NCH>(row)) * 16) + (c & 1) * 8;
+                trans[dt] = row * S::RB + (((2 * dt + ((c & 3) >> 1)) ^ swz<T, S::NCH>(row)) * 16) + (c & 1) * 8;
             } else {
-                trans[dt] = 4 * g * S::RB + (((4 * dt + (c >> 2)) ^ swz<S::NCH>(4 * g)) * 16) + (c & 3) * 4;
+                trans[dt] = 4 * g * S::RB + (((4 * dt + (c >> 2)) ^ swz<T, S::NCH>(4 * g)) * 16) + (c & 3) * 4;
             }
         }
     }
@@ -253,85 +205,61 @@ template <typename T, int DP> struct Reader {
     }
 };
 
-// acc[dt] += (streamed tile transposed) . w, the w of a first product's layout.
+// acc[dt] += (streamed tile transposed) . w, the w of a first product's layout.  Fragments are read one group ahead of the
+// products that take them; the barriers keep the compiler from reading all of them at once, for want of registers.
 template <typename T, int DP>
 __device__ __forceinline__ void second_product(f32x4 (&acc)[DP / 16], const f32x4 (&w)[4], const Reader<T, DP>& rd,
                                                const unsigned char* tile)
 {
     using S = Shape<T, DP>;
-    if constexpr (sizeof(T) == 2) {
+    constexpr int STEPS = sizeof(T) == 2 ? 2 : 4;              // pieces of the 64 rows
+    constexpr int G = S::DT < 4 ? S::DT : 4, PER = S::DT / G, N = STEPS * PER;
+    u32x4 f[2][G];
+    auto read = [&](int n, u32x4 (&to)[G]) {
 #pragma unroll
-        for (int tp = 0; tp < 2; ++tp) {
-            // rounded to nearest even as they enter the matrix cores, whose other operand has as few bits
-            const u32x4 b = {pack_bf16x2(w[2 * tp][0], w[2 * tp][1]), pack_bf16x2(w[2 * tp][2], w[2 * tp][3]),
-                             pack_bf16x2(w[2 * tp + 1][0], w[2 * tp + 1][1]), pack_bf16x2(w[2 * tp + 1][2], w[2 * tp + 1][3])};
-#pragma unroll
-            for (int dt = 0; dt < S::DT; ++dt) {
-                acc[dt] = mma<T>(rd.col_frag2(tile, tp, dt), b, acc[dt]);
-                if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-            }
+        for (int i = 0; i < G; ++i) {
+            if constexpr (sizeof(T) == 2) to[i] = rd.col_frag2(tile, n / PER, (n % PER) * G + i);
+            else to[i] = rd.col_frag1(tile, n / PER, (n % PER) * G + i);
         }
-    } else {
+    };
+    read(0, f[0]);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const u32x4 b = __builtin_bit_cast(u32x4, w[t]);
+    for (int n = 0; n < N; ++n) {
+        if (n + 1 < N) read(n + 1, f[(n + 1) & 1]);
+        const int step = n / PER;
+        u32x4 b;
+        if constexpr (sizeof(T) == 2)       // rounded to nearest even, to as many bits as the other operand has
+            b = u32x4{pack_bf16x2(w[2 * step][0], w[2 * step][1]), pack_bf16x2(w[2 * step][2], w[2 * step][3]),
+                      pack_bf16x2(w[2 * step + 1][0], w[2 * step + 1][1]), pack_bf16x2(w[2 * step + 1][2], w[2 * step + 1][3])};
+        else
+            b = __builtin_bit_cast(u32x4, w[step]);
 #pragma unroll
-            for (int dt = 0; dt < S::DT; ++dt) {
-                acc[dt] = mma<T>(rd.col_frag1(tile, t, dt), b, acc[dt]);
-                if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-            }
-        }
+        for (int i = 0; i < G; ++i) acc[(n % PER) * G + i] = mma<T>(f[n & 1][i], b, acc[(n % PER) * G + i]);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-// first[t] = streamed tile . owner, all 64 rows.
+// first[t] = streamed tile . owner, all 64 rows; the four blocks of rows side by side, since each is one chain of products.
 template <typename T, int DP>
 __device__ __forceinline__ void first_product(f32x4 (&first)[4], const u32x4 (&own)[DP * sizeof(T) / 64], const Reader<T, DP>& rd,
                                               const unsigned char* tile)
 {
     using S = Shape<T, DP>;
+    u32x4 f[2][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         first[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kk = 0; kk < S::KK; ++kk) first[t] = mma<T>(rd.row_frag(tile, t, kk), own[kk], first[t]);
-        if (S::KK >= 4 || t % 2) __builtin_amdgcn_sched_barrier(0);
+        f[0][t] = rd.row_frag(tile, t, 0);
     }
-}
-
-// What second_product leaves out where a tile holds non-finite elements and some pairs of it are masked: the tile went to
-// LDS with zeros in their place, since a zero weight times them would not be zero, and the pairs that are visible take
-// them here from memory.  Rare, so written to be small.
-template <typename T, int DP>
-__device__ __forceinline__ void add_nonfinite(f32x4 (&acc)[DP / 16], const f32x4 (&w)[4], uint32_t vis,
-                                              const T* __restrict__ base, int64_t sr, int rows, int dim)
-{
-    const int c = lane_id() & 15, g = lane_id() >> 4;
-#pragma unroll 1
-    for (int i = 0; i < 16; ++i) {
-        float wi = w[0][0];
 #pragma unroll
-        for (int s = 1; s < 16; ++s) wi = s == i ? w[s >> 2][s & 3] : wi;
-        const int vi = (vis >> i) & 1;
-#pragma unroll 1
-        for (int g2 = 0; g2 < 4; ++g2) {
-            const int row = 16 * (i >> 2) + 4 * g2 + (i & 3);
-            const float wk = __shfl(wi, g2 * 16 + c);
-            const int vk = __shfl(vi, g2 * 16 + c);
-            if (row >= rows) continue;
-            int cols = dim - 4 * g;
-            asm volatile("" : "+v"(cols));       // or 4 DT comparisons are held in registers through the loops
+    for (int kk = 0; kk < S::KK; ++kk) {
+        if (kk + 1 < S::KK) {
 #pragma unroll
-            for (int dt = 0; dt < Shape<T, DP>::DT; ++dt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int col = 16 * dt + 4 * g + e;
-                    if (16 * dt + e < cols && vk) {
-                        const float x = load_elem(base + row * sr + col);
-                        if (nonfinite_bits(__builtin_bit_cast(uint32_t, x))) acc[dt][e] += wk * x;
-                    }
-                }
+            for (int t = 0; t < 4; ++t) f[(kk + 1) & 1][t] = rd.row_frag(tile, t, kk + 1);
         }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) first[t] = mma<T>(f[kk & 1][t], own[kk], first[t]);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -382,6 +310,16 @@ __device__ __forceinline__ float wave_total(float v)
     v = ror(v, std::integral_constant<int, 0x121>{});
     return group_sum(v);
 }
+// Over eight neighbouring lanes.
+__device__ __forceinline__ float eight_lanes_total(float v)
+{
+    auto dpp = [](float x, auto ctrl) {
+        return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    v = dpp(v, std::integral_constant<int, 0xB1>{});        // lane ^ 1
+    v = dpp(v, std::integral_constant<int, 0x4E>{});        // lane ^ 2
+    return dpp(v, std::integral_constant<int, 0x141>{});    // the other four of eight
+}
 __device__ __forceinline__ int wave_max_i(int v)
 {
     return __builtin_amdgcn_readlane(wave_incl_scan_op(v, (int)0x80000000, [](int a, int b) { return a > b ? a : b; }), kWave - 1);
@@ -427,6 +365,15 @@ __device__ __forceinline__ void to_scores(f32x4 (&s)[4], f32x4 (&slope)[CAP ? 4 
     }
 }
 
+// bias: at the lane's first row of the tile.
+__device__ __forceinline__ void add_bias(f32x4 (&s)[4], const float* bias)
+{
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[n][r] += bias[16 * n + r];
+}
+
 // border: the borders in LDS.  The logarithm gives the bucket or one beside it.
 __device__ __forceinline__ int bucket_side(const AttBuckets& bk, const int* border, int n)
 {
@@ -453,10 +400,30 @@ __device__ __forceinline__ int uniform_bucket(const AttBuckets& bk, int lo, int 
 
 // ---- non-finite values ------------------------------------------------------------------------------------
 //
-// A masked pair has weight zero, and zero times an infinity or a NaN of the streamed tile is not zero: a second product would
-// carry such a value to owner rows that do not see it.  A block therefore runs in its common form, which does not care, and
-// looks at its accumulators before it writes: if none holds a non-finite value, no product met one.  Otherwise it starts
-// again in its careful form, which gives the value to the rows that see it and to no others.
+// A masked pair has weight zero, and zero times an infinity or a NaN of the streamed tile is not zero: a product over the
+// tile's rows would carry such a value to owner rows that do not see it.  In tiles with masked pairs a chunk that holds one
+// goes to LDS as zeros, and the row that it belongs to is marked instead: its scores become NaN where they are visible.
+template <typename T> __device__ __forceinline__ bool chunk_nonfinite(u32x4 v)
+{
+    if constexpr (sizeof(T) == 2) {
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 most = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = v[e] & 0x7f807f80u;
+            most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x));
+        }
+        return most[0] == 0x7f80 || most[1] == 0x7f80;
+    } else {
+        uint32_t most = 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = v[e] & 0x7f800000u;
+            most = most > x ? most : x;
+        }
+        return most == 0x7f800000u;
+    }
+}
 
 // ---- walking the streamed rows ----------------------------------------------------------------------------
 
@@ -485,10 +452,11 @@ struct TileMarks {
 // with any row that is not of the one segment all owner rows have.  own: this lane's segment of its owner row, if there.
 __device__ __forceinline__ void mark_tiles(TileMarks& mk, const int* __restrict__ seg, int length, int own, bool there, int t0, int t1)
 {
+    const int lane = lane_id(), wave = wave_id();
     int lo = there && own >= 0 ? own : 0x7fffffff, hi = there && own >= 0 ? own : -1;
     lo = wave_min(lo), hi = wave_max_i(hi);
     int bad = __any(there && own < 0);
-    if (lane_id() == 0) mk.red[wave_id()] = lo, mk.red[4 + wave_id()] = hi, mk.red[8 + wave_id()] = bad;
+    if (lane == 0) mk.red[wave] = lo, mk.red[4 + wave] = hi, mk.red[8 + wave] = bad;
     for (int i = t0 / 32 + threadIdx.x; i <= t1 / 32; i += kBlock)
         if (i < kAttMaxTiles / 32) mk.active[i] = 0u, mk.mixed[i] = 0u;
     __syncthreads();
@@ -499,11 +467,11 @@ __device__ __forceinline__ void mark_tiles(TileMarks& mk, const int* __restrict_
         bad |= mk.red[8 + w];
     }
     const bool one = lo == hi && !bad;
-    for (int t = t0 + wave_id(); t < t1; t += kWavesPerBlock) {
-        const int v = row_segment(seg, t * kTile + lane_id(), length);
+    for (int t = t0 + wave; t < t1; t += kWavesPerBlock) {
+        const int v = row_segment(seg, t * kTile + lane, length);
         const bool touch = __any(v >= lo && v <= hi);
         const bool plain = one && __all(v == lo);
-        if (lane_id() == 0) {
+        if (lane == 0) {
             if (touch) atomicOr(&mk.active[t >> 5], 1u << (t & 31));
             if (!plain) atomicOr(&mk.mixed[t >> 5], 1u << (t & 31));
         }
@@ -534,87 +502,65 @@ __device__ __forceinline__ bool tile_mixed(const TileMarks* mk, int t)
 template <typename T, int DP, int UNIT> struct Feed {
     using S = Shape<T, DP>;
     static constexpr int STEP = kBlock / S::NCH;      // rows between a thread's chunks
+    const int tid;
     u32x4 a[S::NC], b[S::NC];
     int seg;                                          // of row (lane) of the tile
 
+    __device__ __forceinline__ explicit Feed(int thread) : tid(thread), seg(kNoSeg) {}
     // pa, pb: row row0 of the operands
     __device__ __forceinline__ void load(const T* pa, int64_t sa, const T* pb, int64_t sb, int row0, int length,
                                          const int* __restrict__ segments, int dim)
     {
         const RowSource ra = row_source(pa, sa, length - row0, dim), rb = row_source(pb, sb, length - row0, dim);
-        const uint32_t row = threadIdx.x / S::NCH;
-        const int ch = threadIdx.x % S::NCH;
+        const uint32_t row = (uint32_t)tid / S::NCH;
+        const int ch = (uint32_t)tid % S::NCH;
 #pragma unroll
         for (int i = 0; i < S::NC; ++i) {
             a[i] = load_chunk<T, UNIT>(ra, (row + i * STEP) * ra.stride, ch, dim);
             b[i] = load_chunk<T, UNIT>(rb, (row + i * STEP) * rb.stride, ch, dim);
         }
-        seg = row_segment(segments, row0 + lane_id(), length);
+        seg = row_segment(segments, row0 + (tid & (kWave - 1)), length);
     }
-    // CAREFUL, of a tile with masked pairs: non-finite elements of the operands named (those that enter a second product) are
-    // replaced by zeros, and flags[wave] says whether there were any.
-    template <bool CAREFUL, bool A, bool B>
-    __device__ __forceinline__ void put(unsigned char* ta, unsigned char* tb, int* s_seg, bool masked, uint32_t* flags)
+    // masked: the tile has masked pairs.  MARK_A: the mark of a row is a NaN among its elements of a (the operand of the first
+    // product only); else its bit in bad[].
+    template <bool MARK_A>
+    __device__ __forceinline__ void put(unsigned char* ta, unsigned char* tb, int* s_seg, bool masked, uint32_t* bad)
     {
-        const int row = threadIdx.x / S::NCH, ch = threadIdx.x % S::NCH;
+        const int row = (uint32_t)tid / S::NCH, ch = (uint32_t)tid % S::NCH;
         const uint64_t there = __ballot(seg != kNoSeg);
         if (~there) {                                 // padding contributes nothing, whatever it holds
 #pragma unroll
             for (int i = 0; i < S::NC; ++i)
                 if (!((there >> (row + i * STEP)) & 1)) a[i] = b[i] = u32x4{0u, 0u, 0u, 0u};
         }
-        if constexpr (CAREFUL) {
-            bool odd = false;
-            if (masked) {
+        if (masked) {
 #pragma unroll
-                for (int i = 0; i < S::NC; ++i) {
-                    if (A) odd |= clean_chunk<T>(a[i]);
-                    if (B) odd |= clean_chunk<T>(b[i]);
+            for (int i = 0; i < S::NC; ++i) {
+                const bool odd_a = chunk_nonfinite<T>(a[i]), odd_b = chunk_nonfinite<T>(b[i]);
+                if (odd_a || odd_b) {
+                    if (odd_a) a[i] = u32x4{0u, 0u, 0u, 0u};
+                    if (odd_b) b[i] = u32x4{0u, 0u, 0u, 0u};
+                    if (MARK_A) a[i][0] = sizeof(T) == 2 ? 0x7fc0u : 0x7fc00000u;
+                    else if (bad) atomicOr(&bad[(row + i * STEP) >> 5], 1u << ((row + i * STEP) & 31));
                 }
             }
-            odd = __any(odd);
-            if (lane_id() == 0) flags[wave_id()] = odd;
         }
-        if (wave_id() == 0) s_seg[lane_id()] = seg;
+        if ((tid >> 6) == 0) s_seg[(tid & (kWave - 1))] = seg;
 #pragma unroll
         for (int i = 0; i < S::NC; ++i) {
-            const int at = (row + i * STEP) * S::RB + ((ch ^ swz<S::NCH>(row + i * STEP)) * 16);
+            const int at = (row + i * STEP) * S::RB + ((ch ^ swz<T, S::NCH>(row + i * STEP)) * 16);
             *reinterpret_cast<u32x4*>(ta + at) = a[i];
             *reinterpret_cast<u32x4*>(tb + at) = b[i];
         }
     }
 };
 
-__device__ __forceinline__ bool any_flag(const uint32_t* flags)
-{
-    const u32x4 f = *reinterpret_cast<const u32x4*>(flags);
-    return __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]) != 0;
-}
-
-// A tile's masked scores: minus infinity where !(row of the tile in the owner's segment and below `last` [from `first` on]).
-// SEGMENTS: compare the rows' segments, else only their place.
-template <bool SEGMENTS>
-__device__ __forceinline__ uint32_t visible_bits(const int* s_seg, int own, int first, int last)
-{
-    const int g4 = 4 * (lane_id() >> 4);
-    uint32_t vis = 0u;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        typedef int i32x4 __attribute__((ext_vector_type(4)));
-        i32x4 sg = {0, 0, 0, 0};
-        if (SEGMENTS) sg = *reinterpret_cast<const i32x4*>(s_seg + 16 * n + g4);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const bool see = (!SEGMENTS || sg[r] == own) && 16 * n + r < last - g4 && 16 * n + r >= first - g4;
-            vis |= see ? 1u << (4 * n + r) : 0u;
-        }
-    }
-    return vis;
-}
+// A tile's masked scores: minus infinity where the row of the tile is not in the owner's segment (SEGMENTS; else only the
+// place counts) or not below `edge` (FROM: from `edge` on).
 template <bool SEGMENTS, bool FROM>
-__device__ __forceinline__ void mask_scores(f32x4 (&s)[4], const int* s_seg, int own, int edge)
+__device__ __forceinline__ void mask_scores(f32x4 (&s)[4], const int* s_seg, int own, int edge, int lane)
 {
-    const int g4 = 4 * (lane_id() >> 4);
+    const int g4 = 4 * (lane >> 4);
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -630,10 +576,11 @@ __device__ __forceinline__ void mask_scores(f32x4 (&s)[4], const int* s_seg, int
 
 // Owner fragments: row c of the wave's 16, zeros where the row is padding or not there.
 template <typename T, int DP, int UNIT>
-__device__ __forceinline__ void load_owner(u32x4 (&f)[DP * sizeof(T) / 64], const T* base, int64_t sr, int rows, int dim, bool live)
+__device__ __forceinline__ void load_owner(u32x4 (&f)[DP * sizeof(T) / 64], const T* base, int64_t sr, int rows, int dim, bool live,
+                                           int lane)
 {
     const RowSource src = row_source(base, sr, rows < 16 ? rows : 16, dim);
-    const int c = lane_id() & 15, g = lane_id() >> 4;
+    const int c = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int kk = 0; kk < Shape<T, DP>::KK; ++kk) {
         f[kk] = load_chunk<T, UNIT>(src, (uint32_t)c * src.stride, g + 4 * kk, dim);
@@ -641,19 +588,50 @@ __device__ __forceinline__ void load_owner(u32x4 (&f)[DP * sizeof(T) / 64], cons
     }
 }
 
-// Whether a non-finite value is among a wave's accumulators.
-template <int N> __device__ __forceinline__ bool any_nonfinite(const f32x4 (&acc)[N])
+// A wave's 16 owner rows (lane (c, g): row c, columns 16 dt + 4 g + r) times `scale`, to memory.  They pass through the
+// wave's own rows of LDS, so that a store covers whole rows: straight from the accumulators it would write 32 bytes (bf16) of
+// 16 rows, which took the pass over the keys a quarter longer (1.32 against 1.06 ms without stores on 1024 x 200, 8 heads of
+// 128).  room: 16 rows of LDS that no wave reads any more.
+template <typename T, int DP, int UNIT>
+__device__ __forceinline__ void store_rows(unsigned char* room, const f32x4 (&acc)[DP / 16], float scale, T* base, int64_t sr, int rows, int dim,
+                                           int lane)
 {
-    uint32_t most = 0u;
+    using S = Shape<T, DP>;
+    const int c = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float v = acc[i][r];
-            const uint32_t e = __builtin_bit_cast(uint32_t, v) & 0x7f800000u;
-            most = most > e ? most : e;
+    for (int dt = 0; dt < S::DT; ++dt) {
+        const f32x4 v = acc[dt] * scale;
+        if constexpr (sizeof(T) == 2) {
+            const u32x2 h = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+            *reinterpret_cast<u32x2*>(room + c * S::RB + (((2 * dt + (g >> 1)) ^ swz<T, S::NCH>(c)) * 16) + (g & 1) * 8) = h;
+        } else {
+            *reinterpret_cast<f32x4*>(room + c * S::RB + (((4 * dt + g) ^ swz<T, S::NCH>(c)) * 16)) = v;
         }
-    return nonfinite_bits(most);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    constexpr int EPC = 16 / sizeof(T), ROWS = kWave / S::NCH;             // rows per pass of the wave
+#pragma unroll
+    for (int i = 0; i < 16 / ROWS; ++i) {
+        const int row = i * ROWS + lane / S::NCH, ch = lane % S::NCH, at = ch * EPC;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(room + row * S::RB + ((ch ^ swz<T, S::NCH>(row)) * 16));
+        if (row >= rows || at >= dim) continue;
+        T* const to = base + row * sr + at;
+        if constexpr (UNIT == 16) {
+            *reinterpret_cast<u32x4*>(to) = v;
+        } else if constexpr (UNIT == 8) {
+            *reinterpret_cast<u32x2*>(to) = u32x2{v[0], v[1]};
+            if (at + 4 < dim) *reinterpret_cast<u32x2*>(to + 4) = u32x2{v[2], v[3]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < EPC; ++e)
+                if (at + e < dim) {
+                    if constexpr (sizeof(T) == 2) to[e].bits = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
+                    else to[e] = as_f32(v[e]);
+                }
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------

@@ -11,23 +11,37 @@ template <typename T, int DP> struct DkvShared {
     __attribute__((aligned(1024))) unsigned char q[Shape<T, DP>::TILE], d[Shape<T, DP>::TILE];
     __attribute__((aligned(16))) int seg[kTile];
     __attribute__((aligned(16))) float lse[kTile], delta[kTile];
-    __attribute__((aligned(16))) uint32_t flags[4];
+    uint32_t bad[2][2];                            // rows of a tile (by parity) that are marked
     float bias[2 * kTile];
     int border[kMaxBorders];
     TileMarks marks;
 };
 
+// NaN in the scores of marked rows.
+__device__ __forceinline__ void spoil_rows(f32x4 (&s)[4], const uint32_t* bad, int g)
+{
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if ((bad[n >> 1] >> (16 * (n & 1) + 4 * g + r)) & 1) s[n][r] = NAN;
+}
+
 // One block: 64 keys of one key head, 16 to a wave, against the queries of all heads of its group, one head after the
-// other.  False as for attend_block.
-template <typename T, int DP, int UNIT, bool CAP, bool CAREFUL>
-__device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh, int item)
+// other.
+template <typename T, int DP, int UNIT, bool CAP, int WAVES>
+__global__ __launch_bounds__(kBlock, WAVES) void k_attend_dkv(const AttArgs a)
 {
     using S = Shape<T, DP>;
-    constexpr bool AHEAD = !CAREFUL && S::RB < 256;
+    constexpr bool AHEAD = S::RB < 256;
+    __shared__ DkvShared<T, DP> sh;
+    const int item = xcd_item(a.items);
+    if (item < 0) return;
+    const int tid = threadIdx.x, lane = lane_id();
     const int ntiles = (a.length + kTile - 1) / kTile;
     const int kt = item % ntiles;
     const int kvh = (item / ntiles) % a.kv_heads, batch = item / ntiles / a.kv_heads;
-    const int c = lane_id() & 15, g = lane_id() >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int k0 = kt * kTile, wk0 = k0 + wave * 16, k = wk0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
     const int prefix = a.prefix ? a.prefix[batch] : 0;
@@ -36,26 +50,21 @@ __device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh
     const int kseg = k < a.length ? row_segment(seg, k, a.length) : kNoSegOwner;
     const bool live = kseg >= 0;
     load_owner<T, DP, UNIT>(kf, static_cast<const T*>(a.k.data) + batch * a.k.sb + kvh * a.k.sh + wk0 * a.k.sr, a.k.sr,
-                            a.length - wk0, a.dim, live);
+                            a.length - wk0, a.dim, live, lane);
     load_owner<T, DP, UNIT>(vf, static_cast<const T*>(a.v.data) + batch * a.v.sb + kvh * a.v.sh + wk0 * a.v.sr, a.v.sr,
-                            a.length - wk0, a.dim, live);
+                            a.length - wk0, a.dim, live, lane);
     const int own = live ? kseg : kNoSegOwner;
     const int t0 = a.causal && k0 >= prefix ? kt : 0;
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
-    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = kernel_borders()[threadIdx.x];
+    if (tid < kMaxBorders) sh.border[tid] = kernel_borders()[tid];
     if (seg) mark_tiles(sh.marks, seg, a.length, kseg, k < a.length, t0, ntiles);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;
 
-    const Reader<T, DP> rd;
-    Feed<T, DP, UNIT> feed;
+    const Reader<T, DP> rd(lane);
+    Feed<T, DP, UNIT> feed(tid);
     float row_lse = 0.f, row_delta = 0.f;
-    f32x4 dk[S::DT], dv[S::DT];
-#pragma unroll
-    for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float z2 = a.scale * kLog2e, zc = CAP ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
     const int first = a.causal && k >= prefix ? k : 0;            // queries from it on see the key, segments aside
-
-    const bool causal_bias = a.causal && prefix <= 0;             // as in the pass over the queries
     // whether all pairs of the query tile with keys up to `row` are visible
     auto whole = [&](int t, int row, bool mixed) {
         const int q0 = t * kTile;
@@ -66,99 +75,83 @@ __device__ __forceinline__ bool dkv_block(const AttArgs& a, DkvShared<T, DP>& sh
     };
     auto load = [&](int h, int t) {
         feed.load(query_rows(a.q, h, t), a.q.sr, query_rows(a.dout, h, t), a.dout.sr, t * kTile, a.length, seg, a.dim);
-        const int row = t * kTile + lane_id();
+        const int row = t * kTile + lane;
         const int64_t stat = ((int64_t)batch * a.heads + kvh * a.group + h) * a.length + (row < a.length ? row : a.length - 1);
         row_lse = a.lse[stat], row_delta = a.delta[stat];
     };
 
+    f32x4 dk[S::DT], dv[S::DT];
+#pragma unroll
+    for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (tid < 4) (&sh.bad[0][0])[tid] = 0u;
+    int parity = 0;
     int h = 0, t = next_tile(t0, ntiles, mk);
     if (AHEAD && t < ntiles) load(0, t);
     while (t < ntiles) {
         if (!AHEAD) load(h, t);
         const bool mixed = tile_mixed(mk, t);
-        const int q0 = t * kTile, lo = q0 - (k0 + kTile - 1);     // the smallest distance of the block's pairs
+        const int q0 = t * kTile, lo = q0 - (k0 + kTile - 1); // the smallest distance of the block's pairs
         const int flat = a.bk.side ? uniform_bucket(a.bk, lo, lo + 2 * kTile - 2) : 0;
         const float* const table = a.table + (int64_t)(kvh * a.group + h) * buckets;
-        const float lse2 = row_lse == -INFINITY ? 0.f : row_lse * kLog2e;
         __syncthreads();
-        feed.template put<CAREFUL, true, true>(sh.q, sh.d, sh.seg, CAREFUL && !whole(t, k0 + kTile - 1, mixed), sh.flags);
-        if (wave_id() == 0) sh.lse[lane_id()] = lse2, sh.delta[lane_id()] = feed.seg == kNoSeg ? 0.f : row_delta;
-        if (flat < 0 && (int)threadIdx.x < 2 * kTile - 1)
-            sh.bias[threadIdx.x] = causal_bias && lo + (int)threadIdx.x < 0 ? -INFINITY : table[bucket_of(a.bk, sh.border, lo + (int)threadIdx.x)] * kLog2e;
+        const bool masked = !whole(t, k0 + kTile - 1, mixed);
+        feed.template put<false>(sh.q, sh.d, sh.seg, masked, sh.bad[parity]);
+        if (wave == 0) {
+            // a query whose statistics are not finite sees a non-finite value; it is marked like one that holds it
+            float lse2 = row_lse == -INFINITY || feed.seg == kNoSeg ? 0.f : row_lse * kLog2e, dl = feed.seg == kNoSeg ? 0.f : row_delta;
+            if (masked && (!(fabsf(lse2) < INFINITY) || !(fabsf(dl) < INFINITY))) {
+                lse2 = dl = 0.f;
+                atomicOr(&sh.bad[parity][lane >> 5], 1u << (lane & 31));
+            }
+            sh.lse[lane] = lse2;
+            sh.delta[lane] = dl;
+            if (lane < 2) sh.bad[parity ^ 1][lane] = 0u;          // last read before the barrier above
+        }
+        if (flat < 0 && tid < 2 * kTile - 1)
+            sh.bias[tid] = table[bucket_of(a.bk, sh.border, lo + tid)] * kLog2e;
         int hn = h, tn = next_tile(t + 1, ntiles, mk);
         if (tn >= ntiles && h + 1 < a.group) hn = h + 1, tn = next_tile(t0, ntiles, mk);
         if (AHEAD && tn < ntiles) load(hn, tn);
         __syncthreads();
-        const bool odd = CAREFUL && any_flag(sh.flags);
-        if (wk0 < a.length && !(a.causal && q0 + kTile - 1 < wk0 && wk0 >= prefix)) {
+        const bool sees = wk0 < a.length && !(a.causal && q0 + kTile - 1 < wk0 && wk0 >= prefix);
+        if (sees) {
             f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
             first_product<T, DP>(s, kf, rd, sh.q);
-            const float flat2 = a.bk.side && flat >= 0 ? table[flat] * kLog2e : 0.f;
-            to_scores<CAP>(s, slope, zc, cap2, z2, flat2);
-            if (flat < 0) {
-                const float* const bias = &sh.bias[4 * g - (k - k0) + kTile - 1];
+            to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? table[flat] * kLog2e : 0.f);
+            if (flat < 0) add_bias(s, &sh.bias[4 * g - (k - k0) + kTile - 1]);
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[n][r] += bias[16 * n + r];
-            }
-            uint32_t vis = 0xffffu;
-            if (!whole(t, wk0 + 15, mixed) && !(causal_bias && flat < 0 && !mixed)) {
-                if (CAREFUL) vis = visible_bits<true>(sh.seg, own, first - q0, kTile);
-                if (mixed) mask_scores<true, true>(s, sh.seg, own, first - q0);
-                else mask_scores<false, true>(s, sh.seg, own, first - q0);
+            for (int n = 0; n < 4; ++n) s[n] -= *reinterpret_cast<const f32x4*>(&sh.lse[16 * n + 4 * g]);
+            if (!whole(t, wk0 + 15, mixed)) {
+                if (sh.bad[parity][0] | sh.bad[parity][1]) spoil_rows(s, sh.bad[parity], g);
+                if (mixed) mask_scores<true, true>(s, sh.seg, own, first - q0, lane);
+                else mask_scores<false, true>(s, sh.seg, own, first - q0, lane);
             }
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const f32x4 l = *reinterpret_cast<const f32x4*>(&sh.lse[16 * n + 4 * g]);
+            for (int n = 0; n < 4; ++n)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - l[r]);
-                    if (CAREFUL && !((vis >> (4 * n + r)) & 1)) s[n][r] = 0.f;
-                }
-            }
-            second_product<T, DP>(dv, s, rd, sh.d);
-            if (CAREFUL && odd)
-                add_nonfinite<T, DP>(dv, s, vis, query_rows(a.dout, h, t), a.dout.sr, a.length - q0, a.dim);
+                for (int r = 0; r < 4; ++r) s[n][r] = __builtin_amdgcn_exp2f(s[n][r]);
             first_product<T, DP>(dp, vf, rd, sh.d);
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 const f32x4 dl = *reinterpret_cast<const f32x4*>(&sh.delta[16 * n + 4 * g]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[n][r] *= dp[n][r] - dl[r];
-                    if (CAREFUL && !((vis >> (4 * n + r)) & 1)) s[n][r] = 0.f;
-                }
-                if constexpr (CAP) s[n] *= slope[n];
+                for (int r = 0; r < 4; ++r) dp[n][r] = s[n][r] * (dp[n][r] - dl[r]);
+                if constexpr (CAP) dp[n] *= slope[n];
             }
-            second_product<T, DP>(dk, s, rd, sh.q);
-            if (CAREFUL && odd) add_nonfinite<T, DP>(dk, s, vis, query_rows(a.q, h, t), a.q.sr, a.length - q0, a.dim);
+            second_product<T, DP>(dv, s, rd, sh.d);
+            second_product<T, DP>(dk, dp, rd, sh.q);
         }
+        parity ^= 1;
         h = hn, t = tn;
     }
-
-    if (!CAREFUL && __syncthreads_or(any_nonfinite(dk) || any_nonfinite(dv))) return false;
-    if (k < a.length) {
-        T* const dkp = static_cast<T*>(a.dk.data) + batch * a.dk.sb + kvh * a.dk.sh + k * a.dk.sr;
-        T* const dvp = static_cast<T*>(a.dv.data) + batch * a.dv.sb + kvh * a.dv.sh + k * a.dv.sr;
-#pragma unroll
-        for (int dt = 0; dt < S::DT; ++dt) {
-            store4<T, UNIT>(dkp, 16 * dt + 4 * g, a.dim, dk[dt] * a.scale);
-            store4<T, UNIT>(dvp, 16 * dt + 4 * g, a.dim, dv[dt]);
-        }
-    }
-    return true;
-}
-
-template <typename T, int DP, int UNIT, bool CAP, int WAVES>
-__global__ __launch_bounds__(kBlock, WAVES) void k_attend_dkv(const AttArgs a)
-{
-    __shared__ DkvShared<T, DP> sh;
-    const int item = xcd_item(a.items);
-    if (item < 0) return;
-    if (dkv_block<T, DP, UNIT, CAP, false>(a, sh, item)) return;
     __syncthreads();
-    dkv_block<T, DP, UNIT, CAP, true>(args_again(), sh, item);
+    if (wk0 < a.length) {
+        T* const dkp = static_cast<T*>(a.dk.data) + batch * a.dk.sb + kvh * a.dk.sh + wk0 * a.dk.sr;
+        T* const dvp = static_cast<T*>(a.dv.data) + batch * a.dv.sb + kvh * a.dv.sh + wk0 * a.dv.sr;
+        unsigned char* const room = sh.q + wave * 16 * S::RB;
+        store_rows<T, DP, UNIT>(room, dk, a.scale, dkp, a.dk.sr, a.length - wk0, a.dim, lane);
+        store_rows<T, DP, UNIT>(room, dv, 1.f, dvp, a.dv.sr, a.length - wk0, a.dim, lane);
+    }
 }
 
 }  // namespace
@@ -168,7 +161,7 @@ void attend_backward_keys(const gram_attention_config& c, AttArgs a, int unit, h
     a.items = a.batch * a.kv_heads * att_blocks(a.length, kTile);
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
-        constexpr int WAVES = Shape<decltype(type), DP>::RB <= 256 ? 3 : 2;
+        constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 3 : 2;
         k_attend_dkv<decltype(type), DP, decltype(u)::value, decltype(cap)::value, WAVES><<<att_grid(a.items), dim3(kBlock), 0, s>>>(a);
     });
 }

@@ -19,7 +19,6 @@ constexpr int kStrip = 92;       // distances of a wave's 16 queries and a tile'
 template <typename T, int DP> struct DqShared {
     __attribute__((aligned(1024))) unsigned char k[Shape<T, DP>::TILE], v[Shape<T, DP>::TILE];
     __attribute__((aligned(16))) int seg[kTile];
-    __attribute__((aligned(16))) uint32_t flags[4];
     float bias[2 * kTile];
     float table[kMaxBorders];
     int border[kMaxBorders];
@@ -41,17 +40,17 @@ template <int SHIFT> __device__ __forceinline__ float row_shift(float v)        
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
 
-__device__ __forceinline__ void add_bucket(float* bucket, int b, float lane_sums)
+__device__ __forceinline__ void add_bucket(float* bucket, int b, float lane_sums, int lane)
 {
     const float sum = wave_total(lane_sums);
-    if (lane_id() == 0) bucket[b] += sum;
+    if (lane == 0) bucket[b] += sum;
 }
 
 // top: the distance of the wave's first query and the tile's first key.
 __device__ __forceinline__ void table_near(const AttArgs& a, const f32x4 (&ds)[4], int top, float (*strip)[kStrip], float* dist,
-                                           float* bucket, const int* border)
+                                           float* bucket, const int* border, int lane)
 {
-    const int c = lane_id() & 15, g = lane_id() >> 4;
+    const int c = lane & 15, g = lane >> 4;
     float spill = 0.f;
     // distance top + c - 4 g - 16 n lies at place c - 4 g - 16 n + 76 of its group's row
     float* const at = &strip[g][c - 4 * g + 76];
@@ -66,39 +65,43 @@ __device__ __forceinline__ void table_near(const AttArgs& a, const f32x4 (&ds)[4
     float sum[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int place = lane_id() + 64 * h;
+        const int place = lane + 64 * h;
         sum[h] = 0.f;
         if (place < kStrip) sum[h] = (strip[0][place] + strip[1][place]) + (strip[2][place] + strip[3][place]);
     }
     __builtin_amdgcn_wave_barrier();
     const int n0 = top - 76;                                   // distance of place 0
     if (n0 >= -kNear && n0 + kStrip - 1 <= kNear) {
-        dist[n0 + lane_id()] += sum[0];
-        if (lane_id() + 64 < kStrip) dist[n0 + 64 + lane_id()] += sum[1];
+        dist[n0 + lane] += sum[0];
+        if (lane + 64 < kStrip) dist[n0 + 64 + lane] += sum[1];
     } else {
-        const int b0 = bucket_of(a.bk, border, n0 + lane_id()), b1 = bucket_of(a.bk, border, n0 + 64 + lane_id());
-        uint64_t left0 = ~0ull, left1 = __ballot(lane_id() + 64 < kStrip);
+        const int b0 = bucket_of(a.bk, border, n0 + lane), b1 = bucket_of(a.bk, border, n0 + 64 + lane);
+        uint64_t left0 = ~0ull, left1 = __ballot(lane + 64 < kStrip);
         while (left0 | left1) {
             const int b = left0 ? __builtin_amdgcn_readlane(b0, __builtin_ctzll(left0)) : __builtin_amdgcn_readlane(b1, __builtin_ctzll(left1));
-            const bool m0 = b0 == b, m1 = lane_id() + 64 < kStrip && b1 == b;
-            add_bucket(bucket, b, (m0 ? sum[0] : 0.f) + (m1 ? sum[1] : 0.f));
+            const bool m0 = b0 == b, m1 = lane + 64 < kStrip && b1 == b;
+            add_bucket(bucket, b, (m0 ? sum[0] : 0.f) + (m1 ? sum[1] : 0.f), lane);
             left0 &= ~__ballot(m0), left1 &= ~__ballot(m1);
         }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// One block: 64 queries of one head; false as for attend_block.  dist: kWavesPerBlock rows of 2 kNear + 1 sums of ds by
-// distance.
-template <typename T, int DP, int UNIT, bool CAP, bool CAREFUL>
-__device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, float* dist, int item)
+// One block: 64 queries of one head.  Dynamic LDS: kWavesPerBlock rows of 2 kNear + 1 sums of ds by distance.
+template <typename T, int DP, int UNIT, bool CAP, int WAVES>
+__global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
 {
     using S = Shape<T, DP>;
-    constexpr bool AHEAD = !CAREFUL && S::RB < 256;
+    constexpr bool AHEAD = S::RB < 256;
+    extern __shared__ float dist[];
+    __shared__ DqShared<T, DP> sh;
+    const int item = xcd_item(a.items);
+    if (item < 0) return;
+    const int tid = threadIdx.x, lane = lane_id();
     const int nqt = (a.length + kTile - 1) / kTile;
     const int qt = nqt - 1 - item % nqt;
     const int head = (item / nqt) % a.heads, batch = item / nqt / a.heads, kvh = head / a.group;
-    const int c = lane_id() & 15, g = lane_id() >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int q0 = qt * kTile, wq0 = q0 + wave * 16, q = wq0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
     const int prefix = a.prefix ? a.prefix[batch] : 0;
@@ -111,14 +114,14 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
     const int qseg = q < a.length ? row_segment(seg, q, a.length) : kNoSegOwner;
     const bool live = qseg >= 0;
     load_owner<T, DP, UNIT>(qf, static_cast<const T*>(a.q.data) + batch * a.q.sb + head * a.q.sh + wq0 * a.q.sr, a.q.sr,
-                            a.length - wq0, a.dim, live);
+                            a.length - wq0, a.dim, live, lane);
     load_owner<T, DP, UNIT>(df, static_cast<const T*>(a.dout.data) + batch * a.dout.sb + head * a.dout.sh + wq0 * a.dout.sr,
-                            a.dout.sr, a.length - wq0, a.dim, live);
+                            a.dout.sr, a.length - wq0, a.dim, live, lane);
     float delta = 0.f;
     if (!want_table) {
         u32x4 of[S::KK];
         load_owner<T, DP, UNIT>(of, static_cast<const T*>(a.o.data) + batch * a.o.sb + head * a.o.sh + wq0 * a.o.sr, a.o.sr,
-                                a.length - wq0, a.dim, live);
+                                a.length - wq0, a.dim, live, lane);
 #pragma unroll
         for (int kk = 0; kk < S::KK; ++kk) delta += dot_chunk<T>(df[kk], of[kk]);
         delta = group_sum(delta);
@@ -135,23 +138,14 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
         t1 = t1 < ntiles ? t1 : ntiles;
     }
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
-    if ((int)threadIdx.x < buckets) sh.table[threadIdx.x] = a.table[(int64_t)head * buckets + threadIdx.x] * kLog2e;
-    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = kernel_borders()[threadIdx.x];
-    if (want_table) {
-        for (int i = threadIdx.x; i < kWavesPerBlock * (2 * kNear + 1); i += kBlock) dist[i] = 0.f;
-        for (int i = threadIdx.x; i < kWavesPerBlock * 4 * kStrip; i += kBlock) (&sh.strip[0][0][0])[i] = 0.f;
-        if (threadIdx.x < kMaxBorders)
-            for (int w = 0; w < kWavesPerBlock; ++w) sh.bucket[w][threadIdx.x] = 0.f;
-    }
-    float* const my_dist = dist + wave_id() * (2 * kNear + 1) + kNear;
+    if (tid < buckets) sh.table[tid] = a.table[(int64_t)head * buckets + tid] * kLog2e;
+    if (tid < kMaxBorders) sh.border[tid] = kernel_borders()[tid];
     if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;
+    float* const my_dist = dist + wave * (2 * kNear + 1) + kNear;
 
-    const Reader<T, DP> rd;
-    Feed<T, DP, UNIT> feed;
-    f32x4 dq[S::DT];
-#pragma unroll
-    for (int dt = 0; dt < S::DT; ++dt) dq[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const Reader<T, DP> rd(lane);
+    Feed<T, DP, UNIT> feed(tid);
     const float z2 = a.scale * kLog2e, zc = CAP ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
     int last = a.length;
     if (a.causal) {
@@ -160,10 +154,6 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
     }
     if (q >= a.length) last = 0;                                  // the table's gradient is summed over rows
     const bool full_rows = wq0 + 16 <= a.length;
-    int flat_bucket = -1;
-    float flat_sum = 0.f;
-
-    const bool causal_bias = a.causal && prefix <= 0;             // as in the forward pass
     auto whole = [&](int t, int row, bool mixed) {
         const int k1 = t * kTile + kTile;
         return !mixed && k1 <= a.length && (!a.causal || k1 - 1 <= row || k1 <= prefix);
@@ -172,10 +162,27 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
         const int k0 = t * kTile;
         feed.load(kp + k0 * a.k.sr, a.k.sr, vp + k0 * a.v.sr, a.v.sr, k0, a.length, seg, a.dim);
     };
-
-    // DELTA: only sum p dp; else the gradients, with that sum on the way where the one tile holds it all
     const int tfirst = next_tile(0, t1, mk);
     const bool one_tile = want_table && next_tile(tfirst + 1, t1, mk) >= t1;
+
+    f32x4 dq[S::DT];
+#pragma unroll
+    for (int dt = 0; dt < S::DT; ++dt) dq[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // the distances that the block's pairs can have (table_near touches 76 below a pair of tiles), within kNear
+    const int near_lo = q0 - (t1 - 1) * kTile - 76 > -kNear ? q0 - (t1 - 1) * kTile - 76 : -kNear;
+    const int near_hi = q0 + kTile - 1 < kNear ? q0 + kTile - 1 : kNear;
+    int flat_bucket = -1;
+    float flat_sum = 0.f;
+    if (want_table) {
+        for (int n = near_lo + tid; n <= near_hi; n += kBlock)
+#pragma unroll
+            for (int w = 0; w < kWavesPerBlock; ++w) dist[w * (2 * kNear + 1) + kNear + n] = 0.f;
+        for (int i = tid; i < kWavesPerBlock * 4 * kStrip; i += kBlock) (&sh.strip[0][0][0])[i] = 0.f;
+        if (tid < kMaxBorders)
+            for (int w = 0; w < kWavesPerBlock; ++w) sh.bucket[w][tid] = 0.f;
+        delta = 0.f;
+    }
+    // DELTA: only sum p dp; else the gradients, with that sum on the way where the one tile holds it all
     auto walk = [&](auto delta_only) {
         constexpr bool DELTA = decltype(delta_only)::value;
         int t = tfirst;
@@ -186,49 +193,35 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
             const int flat = a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
             if (!AHEAD) load(t);
             __syncthreads();
-            feed.template put<CAREFUL, true, false>(sh.k, sh.v, sh.seg, CAREFUL && !whole(t, q0, mixed), sh.flags);
-            if (flat < 0 && (int)threadIdx.x < 2 * kTile - 1) {
-                sh.bias[threadIdx.x] = causal_bias && hi < (int)threadIdx.x ? -INFINITY : sh.table[bucket_of(a.bk, sh.border, hi - (int)threadIdx.x)];
-            }
+            feed.template put<false>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
+            if (flat < 0 && tid < 2 * kTile - 1)
+                sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, hi - tid)];
             const int tn = next_tile(t + 1, t1, mk);
             if (AHEAD && tn < t1) load(tn);
             __syncthreads();
-            const bool odd = CAREFUL && any_flag(sh.flags);
-            if (wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix)) {
+            const bool sees = wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix);
+            if (sees) {
                 f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
                 first_product<T, DP>(s, qf, rd, sh.k);
-                const float flat2 = a.bk.side && flat >= 0 ? sh.table[flat] : 0.f;
-                to_scores<CAP>(s, slope, zc, cap2, z2, flat2);
-                if (flat < 0) {
-                    const float* const bias = &sh.bias[4 * g - (q - q0) + kTile - 1];
-#pragma unroll
-                    for (int n = 0; n < 4; ++n)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[n][r] += bias[16 * n + r];
-                }
-                uint32_t vis = 0xffffu;
-                if ((!whole(t, wq0, mixed) && !(causal_bias && flat < 0 && !mixed)) || !full_rows) {
-                    if (CAREFUL && odd) vis = visible_bits<true>(sh.seg, own, 0, last - k0);
-                    if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0);
-                    else mask_scores<false, false>(s, sh.seg, own, last - k0);
+                to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? sh.table[flat] : 0.f);
+                if (flat < 0) add_bias(s, &sh.bias[4 * g - (q - q0) + kTile - 1]);
+                if (!whole(t, wq0, mixed) || !full_rows) {
+                    if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0, lane);
+                    else mask_scores<false, false>(s, sh.seg, own, last - k0, lane);
                 }
                 first_product<T, DP>(dp, df, rd, sh.v);
 #pragma unroll
                 for (int n = 0; n < 4; ++n)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - lse2);
-                        // a masked pair has weight 0; its dp may be anything
-                        if (CAREFUL && !((vis >> (4 * n + r)) & 1)) dp[n][r] = 0.f;
-                    }
-                if (DELTA || one_tile) {
+                    for (int r = 0; r < 4; ++r) s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - lse2);
+                if (DELTA || (want_table && one_tile)) {
 #pragma unroll
                     for (int n = 0; n < 4; ++n)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) delta += s[n][r] * dp[n][r];
                 }
                 if constexpr (!DELTA) {
-                    if (one_tile) delta = group_sum(delta);
+                    if (want_table && one_tile) delta = group_sum(delta);
 #pragma unroll
                     for (int n = 0; n < 4; ++n)
 #pragma unroll
@@ -236,13 +229,13 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
                     if (want_table) {
                         if (flat >= 0) {
                             if (flat != flat_bucket) {
-                                if (flat_bucket >= 0) add_bucket(sh.bucket[wave_id()], flat_bucket, flat_sum);
+                                if (flat_bucket >= 0) add_bucket(sh.bucket[wave], flat_bucket, flat_sum, lane);
                                 flat_bucket = flat, flat_sum = 0.f;
                             }
 #pragma unroll
                             for (int n = 0; n < 4; ++n) flat_sum += (s[n][0] + s[n][1]) + (s[n][2] + s[n][3]);
                         } else {
-                            table_near(a, s, wq0 - k0, sh.strip[wave_id()], my_dist, sh.bucket[wave_id()], sh.border);
+                            table_near(a, s, wq0 - k0, sh.strip[wave], my_dist, sh.bucket[wave], sh.border, lane);
                         }
                     }
                     if constexpr (CAP) {
@@ -250,7 +243,6 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
                         for (int n = 0; n < 4; ++n) s[n] *= slope[n];
                     }
                     second_product<T, DP>(dq, s, rd, sh.k);
-                    if (CAREFUL && odd) add_nonfinite<T, DP>(dq, s, vis, kp + k0 * a.k.sr, a.k.sr, a.length - k0, a.dim);
                 }
             }
             t = tn;
@@ -259,52 +251,36 @@ __device__ __forceinline__ bool dq_block(const AttArgs& a, DqShared<T, DP>& sh, 
     };
     if (want_table && !one_tile) walk(std::true_type{});
     walk(std::false_type{});
-    if (!CAREFUL && __syncthreads_or(any_nonfinite(dq))) return false;
-
-    if (q < a.length) {
-        T* const dqp = static_cast<T*>(a.dq.data) + batch * a.dq.sb + head * a.dq.sh + q * a.dq.sr;
-#pragma unroll
-        for (int dt = 0; dt < S::DT; ++dt) store4<T, UNIT>(dqp, 16 * dt + 4 * g, a.dim, dq[dt] * a.scale);
-        if (g == 0) a.delta[stat] = delta;
+    __syncthreads();
+    if (wq0 < a.length) {
+        T* const dqp = static_cast<T*>(a.dq.data) + batch * a.dq.sb + head * a.dq.sh + wq0 * a.dq.sr;
+        store_rows<T, DP, UNIT>(sh.k + wave * 16 * S::RB, dq, a.scale, dqp, a.dq.sr, a.length - wq0, a.dim, lane);
+        if (g == 0 && q < a.length) a.delta[stat] = delta;
     }
     if (want_table) {
-        if (flat_bucket >= 0) add_bucket(sh.bucket[wave_id()], flat_bucket, flat_sum);
+        if (flat_bucket >= 0) add_bucket(sh.bucket[wave], flat_bucket, flat_sum, lane);
         __syncthreads();
-        // bucket b of a side: the distances from its border to the next one's; keys after the query count as distance 0
-        // where there is one side
-        for (int b = wave_id(); b < buckets; b += kWavesPerBlock) {
+        // bucket b of a side: the distances from its border to the next one's, eight lanes to a bucket; keys after the
+        // query count as distance 0 where there is one side
+        const float* const row = dist + kNear;
+        constexpr int W = 2 * kNear + 1;
+        auto at = [&](int n) { return (row[n] + row[W + n]) + (row[2 * W + n] + row[3 * W + n]); };
+        for (int b = tid >> 3; b < buckets; b += kBlock / 8) {
+            const int sub = tid & 7;
             const bool after = b >= a.bk.side;
-            const int i = (after ? b - a.bk.side : b) - a.bk.exact;
+            const int i = (after ? b - a.bk.side : b) - a.bk.exact, most = after ? -near_lo : near_hi;
             int from = i < 0 ? i + a.bk.exact : i == 0 ? a.bk.exact : sh.border[i - 1];
             int to = i < 0 ? from + 1 : i < a.bk.borders ? sh.border[i] : kNear + 1;
-            to = to < kNear + 1 ? to : kNear + 1;
+            to = to < most + 1 ? to : most + 1;
             if (after && from == 0) from = 1;
-            const float* const row = dist + kNear;
-            constexpr int W = 2 * kNear + 1;
-            float sum = lane_id() < kWavesPerBlock ? sh.bucket[lane_id()][b] : 0.f;
-            for (int n = from + lane_id(); n < to; n += kWave) {
-                const float* const r = row + (after ? -n : n);
-                sum += (r[0] + r[W]) + (r[2 * W] + r[3 * W]);
-            }
+            float sum = sub < kWavesPerBlock ? sh.bucket[sub][b] : 0.f;
+            for (int n = from + sub; n < to; n += 8) sum += at(after ? -n : n);
             if (b == 0 && !a.bk.two_sided)
-                for (int n = 1 + lane_id(); n <= 2 * kTile; n += kWave) sum += (row[-n] + row[W - n]) + (row[2 * W - n] + row[3 * W - n]);
-            sum = wave_total(sum);
-            if (lane_id() == 0) a.part[((int64_t)head * a.parts + batch * nqt + qt) * buckets + b] = sum;
+                for (int n = 1 + sub; n <= -near_lo; n += 8) sum += at(-n);
+            sum = eight_lanes_total(sum);
+            if (sub == 0) a.part[((int64_t)head * a.parts + batch * nqt + qt) * buckets + b] = sum;
         }
     }
-    return true;
-}
-
-template <typename T, int DP, int UNIT, bool CAP, int WAVES>
-__global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
-{
-    extern __shared__ float s_dist[];
-    __shared__ DqShared<T, DP> sh;
-    const int item = xcd_item(a.items);
-    if (item < 0) return;
-    if (dq_block<T, DP, UNIT, CAP, false>(a, sh, s_dist, item)) return;
-    __syncthreads();
-    dq_block<T, DP, UNIT, CAP, true>(args_again(), sh, s_dist, item);
 }
 
 }  // namespace

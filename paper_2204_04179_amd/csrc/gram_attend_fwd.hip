@@ -14,24 +14,26 @@ namespace {
 template <typename T, int DP> struct FwdShared {
     __attribute__((aligned(1024))) unsigned char k[Shape<T, DP>::TILE], v[Shape<T, DP>::TILE];
     __attribute__((aligned(16))) int seg[kTile];
-    __attribute__((aligned(16))) uint32_t flags[4];
     float bias[2 * kTile];
     float table[kMaxBorders];
     int border[kMaxBorders];
     TileMarks marks;
 };
 
-// One block: 64 queries of one head, 16 to a wave.  False (CAREFUL not set): an accumulator is not finite and nothing has
-// been written.
-template <typename T, int DP, int UNIT, bool CAP, bool CAREFUL>
-__device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>& sh, int item)
+// One block: 64 queries of one head, 16 to a wave.
+template <typename T, int DP, int UNIT, bool CAP, int WAVES>
+__global__ __launch_bounds__(kBlock, WAVES) void k_attend(const AttArgs a)
 {
     using S = Shape<T, DP>;
-    constexpr bool AHEAD = !CAREFUL && S::RB < 256;
+    constexpr bool AHEAD = S::RB < 256;          // the next tile's loads under way while this one is worked on
+    __shared__ FwdShared<T, DP> sh;
+    const int item = xcd_item(a.items);
+    if (item < 0) return;
+    const int tid = threadIdx.x, lane = lane_id();
     const int nqt = (a.length + kTile - 1) / kTile;
     const int qt = nqt - 1 - item % nqt;                 // the longest rows of a causal mask first
     const int head = (item / nqt) % a.heads, batch = item / nqt / a.heads, kvh = head / a.group;
-    const int c = lane_id() & 15, g = lane_id() >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int q0 = qt * kTile, wq0 = q0 + wave * 16, q = wq0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
     const int prefix = a.prefix ? a.prefix[batch] : 0;
@@ -41,7 +43,7 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
     u32x4 qf[S::KK];
     const int qseg = q < a.length ? row_segment(seg, q, a.length) : kNoSegOwner;
     load_owner<T, DP, UNIT>(qf, static_cast<const T*>(a.q.data) + batch * a.q.sb + head * a.q.sh + wq0 * a.q.sr, a.q.sr,
-                            a.length - wq0, a.dim, qseg >= 0);
+                            a.length - wq0, a.dim, qseg >= 0, lane);
     const int own = qseg < 0 ? kNoSegOwner : qseg;
     const int ntiles = (a.length + kTile - 1) / kTile;
     int t1 = ntiles;
@@ -52,26 +54,19 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
         t1 = t1 < ntiles ? t1 : ntiles;
     }
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
-    if ((int)threadIdx.x < buckets) sh.table[threadIdx.x] = a.table[(int64_t)head * buckets + threadIdx.x] * kLog2e;
-    if (threadIdx.x < kMaxBorders) sh.border[threadIdx.x] = kernel_borders()[threadIdx.x];
+    if (tid < buckets) sh.table[tid] = a.table[(int64_t)head * buckets + tid] * kLog2e;
+    if (tid < kMaxBorders) sh.border[tid] = kernel_borders()[tid];
     if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;
 
-    const Reader<T, DP> rd;
-    Feed<T, DP, UNIT> feed;
-    f32x4 o[S::DT];
-    float top = -INFINITY, total = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < S::DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const Reader<T, DP> rd(lane);
+    Feed<T, DP, UNIT> feed(tid);
     const float z2 = a.scale * kLog2e, zc = CAP ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
     int last = a.length;                                 // keys before it are in sight, segments aside
     if (a.causal) {
         last = q + 1 > prefix ? q + 1 : prefix;
         last = last < a.length ? last : a.length;
     }
-
-    // causal, no prefix: the bias is minus infinity at negative distances, and tiles of one segment need no other mask
-    const bool causal_bias = a.causal && prefix <= 0;
     // whether all pairs of the tile with rows from `row` on are visible
     auto whole = [&](int t, int row, bool mixed) {
         const int k1 = t * kTile + kTile;
@@ -82,38 +77,32 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
         feed.load(kp + k0 * a.k.sr, a.k.sr, vp + k0 * a.v.sr, a.v.sr, k0, a.length, seg, a.dim);
     };
 
+    f32x4 o[S::DT];
+    float top = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < S::DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     int t = next_tile(0, t1, mk);
     if (AHEAD && t < t1) load(t);
     while (t < t1) {
         const bool mixed = tile_mixed(mk, t);
-        const int k0 = t * kTile, hi = q0 + kTile - 1 - k0;       // the largest distance of the block's pairs
+        const int k0 = t * kTile, hi = q0 + kTile - 1 - k0;   // the largest distance of the block's pairs
         const int flat = a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
         if (!AHEAD) load(t);
-        __syncthreads();                                          // the tile before has been read
-        feed.template put<CAREFUL, false, true>(sh.k, sh.v, sh.seg, CAREFUL && !whole(t, q0, mixed), sh.flags);
-        if (flat < 0 && (int)threadIdx.x < 2 * kTile - 1)
-            sh.bias[threadIdx.x] = causal_bias && hi < (int)threadIdx.x ? -INFINITY : sh.table[bucket_of(a.bk, sh.border, hi - (int)threadIdx.x)];
+        __syncthreads();                                      // the tile before has been read
+        feed.template put<true>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
+        if (flat < 0 && tid < 2 * kTile - 1)
+            sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, hi - tid)];
         const int tn = next_tile(t + 1, t1, mk);
         if (AHEAD && tn < t1) load(tn);
         __syncthreads();
-        const bool odd = CAREFUL && any_flag(sh.flags);
         if (wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix)) {
             f32x4 s[4], slope[CAP ? 4 : 1];
             first_product<T, DP>(s, qf, rd, sh.k);
-            const float flat2 = a.bk.side && flat >= 0 ? sh.table[flat] : 0.f;
-            to_scores<CAP>(s, slope, zc, cap2, z2, flat2);
-            if (flat < 0) {
-                const float* const bias = &sh.bias[4 * g - (q - q0) + kTile - 1];
-#pragma unroll
-                for (int n = 0; n < 4; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[n][r] += bias[16 * n + r];
-            }
-            uint32_t vis = 0xffffu;
-            if (!whole(t, wq0, mixed) && !(causal_bias && flat < 0 && !mixed)) {
-                if (CAREFUL && odd) vis = visible_bits<true>(sh.seg, own, 0, last - k0);
-                if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0);
-                else mask_scores<false, false>(s, sh.seg, own, last - k0);
+            to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? sh.table[flat] : 0.f);
+            if (flat < 0) add_bias(s, &sh.bias[4 * g - (q - q0) + kTile - 1]);
+            if (!whole(t, wq0, mixed)) {
+                if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0, lane);
+                else mask_scores<false, false>(s, sh.seg, own, last - k0, lane);
             }
             float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
 #pragma unroll
@@ -127,7 +116,7 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
 #pragma unroll
                 for (int dt = 0; dt < S::DT; ++dt) o[dt] *= shrink;
             }
-            const float base = top == -INFINITY ? 0.f : top;      // a row that has seen nothing so far
+            const float base = top == -INFINITY ? 0.f : top;  // a row that has seen nothing so far
 #pragma unroll
             for (int n = 0; n < 4; ++n)
 #pragma unroll
@@ -136,34 +125,18 @@ __device__ __forceinline__ bool attend_block(const AttArgs& a, FwdShared<T, DP>&
                     total += s[n][r];
                 }
             second_product<T, DP>(o, s, rd, sh.v);
-            if (CAREFUL && odd) add_nonfinite<T, DP>(o, s, vis, vp + k0 * a.v.sr, a.v.sr, a.length - k0, a.dim);
         }
         t = tn;
     }
-
     total = group_sum(total);
-    if (!CAREFUL && __syncthreads_or(any_nonfinite(o))) return false;
-    if (q < a.length) {
+    __syncthreads();                                              // the tiles have been read
+    if (wq0 < a.length) {
         const bool empty = top == -INFINITY && total == 0.f;
-        const float inv = empty ? 0.f : 1.f / total;
-        T* const op = static_cast<T*>(a.o.data) + batch * a.o.sb + head * a.o.sh + q * a.o.sr;
-#pragma unroll
-        for (int dt = 0; dt < S::DT; ++dt) store4<T, UNIT>(op, 16 * dt + 4 * g, a.dim, o[dt] * inv);
-        if (a.lse && g == 0)
+        T* const op = static_cast<T*>(a.o.data) + batch * a.o.sb + head * a.o.sh + wq0 * a.o.sr;
+        store_rows<T, DP, UNIT>(sh.k + wave * 16 * S::RB, o, empty ? 0.f : 1.f / total, op, a.o.sr, a.length - wq0, a.dim, lane);
+        if (a.lse && g == 0 && q < a.length)
             a.lse[((int64_t)batch * a.heads + head) * a.length + q] = empty ? -INFINITY : top * kLn2 + logf(total);
     }
-    return true;
-}
-
-template <typename T, int DP, int UNIT, bool CAP, int WAVES>
-__global__ __launch_bounds__(kBlock, WAVES) void k_attend(const AttArgs a)
-{
-    __shared__ FwdShared<T, DP> sh;
-    const int item = xcd_item(a.items);
-    if (item < 0) return;
-    if (attend_block<T, DP, UNIT, CAP, false>(a, sh, item)) return;
-    __syncthreads();
-    attend_block<T, DP, UNIT, CAP, true>(args_again(), sh, item);
 }
 
 }  // namespace

@@ -309,7 +309,7 @@ class HistoryAttention:
         self.heads, self.kv_heads, self.head_dim, self.buckets = int(heads), int(kv_heads), int(head_dim), int(buckets)
         self.dtype = torch.bfloat16 if dtype == BF16 else torch.float32
         self.cfg = GramAttentionConfig(self.heads, self.kv_heads, self.head_dim, int(dtype),
-                                       float(head_dim) ** -0.5 if scale is None else float(scale), float(cap),
+                                       max(float(head_dim), 1.0) ** -0.5 if scale is None else float(scale), float(cap),
                                        1 if causal else 0, self.buckets, int(max_distance), 1 if two_sided else 0)
         self._cfg = C.byref(self.cfg)
         _ck_call(self._lib.gram_attention(self._cfg, 0, 0, None, None, None, None, None, None, None, None, None))

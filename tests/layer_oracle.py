@@ -81,7 +81,7 @@ def attention(q, k, v, *, scale, cap=0.0, causal=True, segments=None, prefix=Non
     o = p @ V
     # a score is off by (D + 8) U of its terms (cap: a tanh off by 4 U of itself, so of |s| too), which moves a weight by
     # that times itself, and its row's sum by at most as much again; sums over L keys and D columns follow
-    rel = (2 * (D + 8) * float((size * see).max() if see.any() else 0.0) + L + D + 64) * U
+    rel = (2 * (D + 8) * float((size * see).detach().max() if see.any() else 0.0) + L + D + 64) * U
     wround = HB if low else U                       # a weight as it enters the second product
     out = dict(o=(o, (wround + rel) * (p @ V.abs()) + half_step(q.dtype) * o.abs()))
     lse = torch.where(any_, top + torch.log(torch.where(any_, total, torch.ones_like(total))), torch.full_like(top, -torch.inf))[..., 0]

@@ -202,3 +202,215 @@ def test_cached_step(dtype, B, cap_rows, H, KV, D, cap, buckets, far, both, firs
     lo.assert_within(O, (o, bound), "o")
     for got, want, what in ((KC, kw, "k_cache"), (VC, vw, "v_cache")):
         assert torch.equal(torch.nan_to_num(got.cpu().float(), 7.0, 8.0, 9.0), torch.nan_to_num(want.float(), 7.0, 8.0, 9.0)), what
+
+
+# ---- values that are not finite ---------------------------------------------------------------------------
+
+ODD = [
+    case("bf16", 2, 150, 2, 1, 64, buckets=32, far=128), case("f32", 2, 70, 2, 2, 20, docs=True, cap=5.0),
+    case("bf16", 1, 200, 2, 2, 128, docs=True, prefix=True), case("bf16", 2, 130, 4, 2, 33, causal=False, docs=True, buckets=16, far=40, both=True),
+    case("f32", 1, 300, 2, 2, 96, docs=True, pad="holes", buckets=8, far=30), case("bf16", 3, 40, 2, 2, 20, pad="tail", buckets=32, far=64),
+]
+
+
+@pytest.mark.parametrize("what", ["k", "v", "q", "do", "all"])
+@pytest.mark.parametrize("c", ODD, ids=name_of)
+def test_non_finite_values_reach_only_those_that_see_them(c, what):
+    """Some positions hold NaN and infinities.  Rows that have nothing to do with them are what they are without them; rows
+    that see them are not finite.  Padding may hold anything."""
+    import torch
+    from paper_2204_04179_amd import gram
+    q, k, v, do, seg, prefix, table = inputs(torch, c, seed=100)
+    B, L = c["B"], c["L"]
+    bad = torch.zeros(B, L, dtype=torch.bool)
+    bad[:, L // 2] = bad[:, (3 * L) // 4] = True
+    clean = [t.clone() for t in (q, k, v, do)]
+    for n, t, z in zip(("q", "k", "v", "do"), (q, k, v, do), clean):
+        if what in (n, "all"):
+            t[bad] = float("nan")
+            t[0, L // 2, :, 0] = float("inf") if n in ("v", "do") else float("nan")
+            z[bad] = 0.0
+        if seg is not None:
+            t[seg < 0] = float("nan")
+            z[seg < 0] = 0.0
+    pad = torch.zeros(B, L, dtype=torch.bool) if seg is None else seg < 0
+    bad &= ~pad
+    want = oracle_of(c, *clean, seg, prefix, table)
+    got = run_gpu(torch, gram, c, q, k, v, do, seg, prefix, table)
+    see = lo.visible(L, seg, c["causal"], prefix, B)[:, 0].expand(B, L, L)          # [B, query, key]
+    holder = bad if what in ("k", "v", "all") else torch.zeros_like(bad)            # positions that spoil who sees them
+    row = (see & holder[:, None, :]).any(2) | (bad if what in ("q", "all") else False)
+    grow = row | (bad if what == "do" else False)                                   # queries without gradients
+    gkey = (see & grow[:, :, None]).any(1) | (holder & ~pad)
+
+    def split(name, spoilt):
+        value, bound = want[name]
+        out = got[name].cpu().to(torch.float64)
+        keep = ~spoilt
+        lo.assert_within(out[keep], (value[keep], bound[keep]), f"{name} of the others")
+        return out
+
+    out = split("o", row)
+    assert not bool(torch.isfinite(out[row & ~pad]).flatten(1).all(1).any()), "o of a query that sees one is finite"
+    split("dq", grow)
+    for n in ("dk", "dv"):
+        out = split(n, gkey)
+    assert bool((out[pad] == 0).all())
+
+
+@pytest.mark.parametrize("far,L,causal,both", [(600, 1300, True, False), (1000, 900, False, True), (700, 2000, False, False)])
+def test_table_gradient_of_distances_beyond_the_near_sums(far, L, causal, both):
+    import torch
+    from paper_2204_04179_amd import gram
+    c = case("f32", 1, L, 1, 1, 16, causal=causal, buckets=64, far=far, both=both)
+    data = inputs(torch, c, seed=7)
+    want = oracle_of(c, *data)
+    got = run_gpu(torch, gram, c, *data)
+    for n in got:
+        lo.assert_within(got[n], want[n], n)
+
+
+def test_gradients_against_differences():
+    """The table's gradient and dv, dk, dq along a random direction against a central difference of the 64-bit forward."""
+    import torch
+    from paper_2204_04179_amd import gram
+    c = case("f32", 1, 37, 2, 1, 12, docs=True, cap=4.0, buckets=8, far=20)
+    q, k, v, do, seg, prefix, table = inputs(torch, c, seed=3)
+    got = run_gpu(torch, gram, c, q, k, v, do, seg, prefix, table)
+
+    def loss(q, k, v, table):
+        o = lo.attention(q, k, v, scale=12 ** -0.5, cap=4.0, segments=seg, prefix=prefix, table=table, far=20)["o"][0]
+        return float((o * do.double()).sum())
+
+    base = [t.double() for t in (q, k, v, table)]
+    for i, n in enumerate(("dq", "dk", "dv", "dtable")):
+        g = torch.Generator().manual_seed(i)
+        way = torch.randn(base[i].shape, generator=g, dtype=torch.float64)
+        h = 1e-4
+        up, down = ([t + (h if j == i else 0.0) * s * way if j == i else t for j, t in enumerate(base)] for s in (1.0, -1.0))
+        slope = (loss(*up) - loss(*down)) / (2 * h)
+        mine = float((got[n].cpu().double() * way).sum())
+        # the difference is off by h^2 times a third derivative of order |slope| and more, float32 by 1e-5 of the sum's terms
+        assert abs(mine - slope) <= 1e-4 * (abs(slope) + float((got[n].cpu().double() * way).abs().sum())), n
+
+
+# ---- as a program uses them -------------------------------------------------------------------------------
+
+
+def test_results_are_the_same_bits_again_on_another_stream_and_in_a_graph():
+    import torch
+    from paper_2204_04179_amd import gram
+    c = case("bf16", 4, 200, 4, 2, 64, docs=True, pad="tail", buckets=32, far=128)
+    q, k, v, do, seg, prefix, table = (None if t is None else t.cuda() for t in inputs(torch, c, seed=11))
+    plan = plan_of(gram, c)
+    B, L, H = c["B"], c["L"], c["H"]
+    x = draw(torch, (B * L, 256), 1, torch.float32).cuda()
+    w, b = draw(torch, (256,), 2, torch.float32).cuda(), draw(torch, (256,), 3, torch.float32).cuda()
+    kc, vc = draw(torch, (B, 1500, 2, 64), 4, torch.bfloat16).cuda(), draw(torch, (B, 1500, 2, 64), 5, torch.bfloat16).cuda()
+    lens = torch.tensor([1499, 700, -1, 0], dtype=torch.int32, device="cuda")
+
+    def buffers():
+        e = lambda *s, dt=torch.float32: torch.full(s, float("nan"), dtype=dt, device="cuda")
+        return dict(o=e(B, L, H, 64, dt=torch.bfloat16), lse=e(B, H, L), dq=e(B, L, H, 64, dt=torch.bfloat16),
+                    dk=e(B, L, 2, 64, dt=torch.bfloat16), dv=e(B, L, 2, 64, dt=torch.bfloat16), dt=e(H, 32),
+                    work=torch.empty(plan.backward_bytes(B, L), dtype=torch.uint8, device="cuda"),
+                    y=e(B * L, 256, dt=torch.bfloat16), st=e(B * L, 2), dx=e(B * L, 256), dw=e(256), db=e(256),
+                    nw=torch.empty(gram.layer_norm_work_bytes(B * L, 256), dtype=torch.uint8, device="cuda"),
+                    so=e(B, H, 64, dt=torch.bfloat16), sw=torch.empty(plan.step_bytes(B, 1500), dtype=torch.uint8, device="cuda"))
+
+    def go(t, stream=None):
+        gram.layer_norm(x, w, b, t["y"], stats=t["st"], segments=seg, stream=stream)
+        gram.layer_norm_backward(x, w, t["st"], t["y"], t["dx"], t["dw"], t["db"], t["nw"], segments=seg, stream=stream)
+        plan.forward(q, k, v, t["o"], lse=t["lse"], segments=seg, prefix=prefix, table=table, stream=stream)
+        plan.backward(q, k, v, t["o"], t["lse"], do, t["dq"], t["dk"], t["dv"], t["work"], segments=seg, prefix=prefix,
+                      table=table, dtable=t["dt"], stream=stream)
+        plan.step(q[:, 0], k[:, 0], v[:, 0], kc, vc, lens, t["so"], t["sw"], table=table, stream=stream)
+
+    names = ("o", "lse", "dq", "dk", "dv", "dt", "y", "st", "dx", "dw", "db", "so")
+    first, second, third = buffers(), buffers(), buffers()
+    go(first)
+    torch.cuda.synchronize()
+    want = {n: first[n].clone() for n in names}
+    same = lambda t, what: [(torch.equal(t[n], want[n]) or pytest.fail(f"{what}: {n}")) for n in names]
+    side = torch.cuda.Stream()
+    go(second, stream=side)                                    # by argument, while another stream is the current one
+    go(first)
+    torch.cuda.synchronize()
+    same(first, "again"), same(second, "another stream")
+    graphs = []
+    for t in (second, third):                                  # two graphs, each with its own work buffers
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            go(t)
+        graphs.append(g)
+    for replay in range(3):
+        for t in (second, third):
+            for n in names:
+                t[n].fill_(float("nan"))
+        for g in graphs:
+            g.replay()
+        go(first)
+        torch.cuda.synchronize()
+        for t in (first, second, third):
+            same(t, f"replay {replay}")
+
+
+def test_a_training_step_of_the_filter_feeds_the_gradient_accumulation():
+    """dedup -> encoder -> positions -> layer norm -> projections -> attention -> loss, and back into the item gradients:
+    each stage by the library, against the same step in 64 bits."""
+    import numpy as np
+    import torch
+    from paper_2204_04179_amd import gram, workloads as wl
+    wk = wl.get("tiny")
+    B, L, d, H = wk.B, wk.L, wk.d, 4
+    ids = torch.from_numpy(wl.ids(wk).reshape(-1)).cuda()
+    X, W = (torch.from_numpy(t).cuda() for t in (wl.features(wk), wl.weights(wk)))
+    g = gram.Gram(gram.make_config(wk.N, wk.d_in, d, wk.M, 1, 0, 0, gram.F32))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    uniq, inv, cnt, u = torch.empty(wk.N, **i32), torch.empty(wk.M, **i32), torch.empty(wk.N, **i32), torch.zeros(1, **i32)
+    U = g.unique(ids, uniq, inv, cnt, u, want_host_u=True)
+    Hp = torch.empty(wk.M, d, device="cuda")
+    g.encode_gather(X, W, uniq, inv, u, wk.M, None, Hp)
+    seg = torch.where(ids == 0, -1, 0).int()
+    ln_w, ln_b = torch.rand(d, device="cuda") + 0.5, torch.randn(d, device="cuda")
+    Wp = torch.randn(d, 3 * d, device="cuda") * d ** -0.5
+    table = torch.randn(H, 8, device="cuda")
+    do = torch.randn(B, L, H, d // H, device="cuda")
+    plan = gram.HistoryAttention(H, H, d // H, dtype=gram.F32, buckets=8, max_distance=12)
+    y, stats = torch.empty_like(Hp), torch.empty(wk.M, 2, device="cuda")
+    gram.layer_norm(Hp, ln_w, ln_b, y, stats=stats, segments=seg)
+    qkv = (y @ Wp).view(B, L, 3 * H, d // H)
+    o, lse = torch.empty(B, L, H, d // H, device="cuda"), torch.empty(B, H, L, device="cuda")
+    q, k, v = (qkv[:, :, i * H:(i + 1) * H] for i in range(3))
+    plan.forward(q, k, v, o, lse=lse, segments=seg, table=table)
+    dqkv, dtable = torch.empty_like(qkv), torch.empty_like(table)
+    work = torch.empty(plan.backward_bytes(B, L), dtype=torch.uint8, device="cuda")
+    plan.backward(q, k, v, o, lse, do, *(dqkv[:, :, i * H:(i + 1) * H] for i in range(3)), work, segments=seg, table=table,
+                  dtable=dtable)
+    dH, dw, db = torch.empty_like(Hp), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    nw = torch.empty(gram.layer_norm_work_bytes(wk.M, d), dtype=torch.uint8, device="cuda")
+    dy = (dqkv.view(wk.M, 3 * d) @ Wp.T).contiguous()
+    gram.layer_norm_backward(Hp, ln_w, stats, dy, dH, dw, db, nw, segments=seg)
+    g.grad_accumulate(dH, wk.M, 0)
+    G = torch.empty(wk.N, d, device="cuda")
+    n = g.flush(uniq, cnt, G, None, want_host_u=True)
+    assert n == U
+    g.close()
+
+    f = lambda t: t.detach().cpu().double()
+    E = (f(X)[f(ids).long()] @ f(W)) * (f(ids) != 0)[:, None]
+    E.requires_grad_()
+    xh = (E - E.mean(1, keepdim=True)) / torch.sqrt(E.var(1, correction=0, keepdim=True) + 1e-5)
+    yy = (xh * f(ln_w) + f(ln_b)) * (f(seg) >= 0)[:, None]
+    p = (yy @ f(Wp)).view(B, L, 3 * H, d // H)
+    ref = lo.attention(*(p[:, :, i * H:(i + 1) * H] for i in range(3)), scale=(d // H) ** -0.5, segments=seg.cpu().view(B, L),
+                       table=f(table), far=12)["o"][0]
+    (ref * f(do)).sum().backward()
+    per_item = torch.zeros(wk.N, d, dtype=torch.float64).index_add_(0, f(ids).long(), E.grad)
+    per_item[0] = 0.0
+    got = torch.zeros(wk.N, d, dtype=torch.float64)
+    got[uniq[:n].cpu().long()] = f(G[:n])
+    got[0] = 0.0
+    # float32 throughout: sums of at most a few hundred products a stage, amplified by 1 / sigma of the layer norm (~ 1)
+    assert float((got - per_item).abs().max()) <= 2e-5 * float(per_item.abs().max()) and bool(torch.isfinite(got).all())
+    np.testing.assert_allclose(f(o).numpy(), ref.detach().numpy(), rtol=0, atol=2e-5 * float(ref.abs().max()))
