@@ -234,6 +234,8 @@ int gram_attention_step(const gram_attention_config* cfg, int32_t batch, int32_t
                   rvc = u.add(v_cache, es), ro = u.add(o, es);
     const bool null = !lengths || (cfg->buckets > 0 && !table) || (!work && step_part_bytes(*cfg, batch, capacity) > 0);
     if (const char* why = null ? "NULL pointer" : u.refusal(es)) return fail_call(GRAM_ERR_ARG, "gram_attention_step: %s", why);
+    if (rq.sh * es >= kAttMaxRowBytes)      // the heads of a query are the rows of an operand
+        return fail_call(GRAM_ERR_ARG, "gram_attention_step: the heads of q must be less than 64 MiB apart");
     if ((reinterpret_cast<uintptr_t>(work) & 15) != 0)
         return fail_call(GRAM_ERR_ARG, "gram_attention_step: work must be 16-byte aligned");
     AttBuckets bk;

@@ -22,41 +22,44 @@ typedef uint32_t nu32x4 __attribute__((ext_vector_type(4)));
 
 struct bf16_t { uint16_t bits; };
 
-__device__ __forceinline__ float widen(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
-
-template <int VEC> __device__ __forceinline__ void load_vec(const float* __restrict__ p, float* v)
-{
-    if constexpr (VEC == 1) {
-        v[0] = *p;
-    } else {
-#pragma unroll
-        for (int q = 0; q < VEC / 4; ++q) {
-            const nf32x4 t = reinterpret_cast<const nf32x4*>(p)[q];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * q + e] = t[e];
-        }
-    }
-}
-
-template <int VEC> __device__ __forceinline__ void load_vec(const bf16_t* __restrict__ p, float* v)
-{
-    if constexpr (VEC == 1) {
-        v[0] = widen(p->bits);
-    } else {
-        uint32_t t[VEC / 2];
-        if constexpr (VEC == 4) {
-            const nu32x2 u = *reinterpret_cast<const nu32x2*>(p);
-            t[0] = u[0], t[1] = u[1];
+// VEC neighbouring elements as they lie in memory: 16 bytes per load, 8 for four of bf16.
+template <typename T, int VEC> struct Raw {
+    static constexpr int WORDS = VEC * (int)sizeof(T) / 4 > 0 ? VEC * (int)sizeof(T) / 4 : 1;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const T* __restrict__ p)
+    {
+        if constexpr (VEC == 1) {
+            if constexpr (sizeof(T) == 2) w[0] = p->bits;
+            else w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else if constexpr (WORDS == 2) {
+            const nu32x2 t = *reinterpret_cast<const nu32x2*>(p);
+            w[0] = t[0], w[1] = t[1];
         } else {
-            const nu32x4 u = *reinterpret_cast<const nu32x4*>(p);
-            t[0] = u[0], t[1] = u[1], t[2] = u[2], t[3] = u[3];
-        }
 #pragma unroll
-        for (int q = 0; q < VEC / 2; ++q) {
-            v[2 * q] = __builtin_bit_cast(float, t[q] << 16);
-            v[2 * q + 1] = __builtin_bit_cast(float, t[q] & 0xffff0000u);
+            for (int q = 0; q < WORDS / 4; ++q) {
+                const nu32x4 t = reinterpret_cast<const nu32x4*>(p)[q];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[4 * q + e] = t[e];
+            }
         }
     }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int q = 0; q < WORDS; ++q) w[q] = 0u;
+    }
+    __device__ __forceinline__ float get(int e) const
+    {
+        if constexpr (sizeof(T) == 2) return __builtin_bit_cast(float, e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+        else return __builtin_bit_cast(float, w[e]);
+    }
+};
+template <int VEC, typename T> __device__ __forceinline__ void load_vec(const T* __restrict__ p, float* v)
+{
+    Raw<T, VEC> r;
+    r.load(p);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = r.get(e);
 }
 
 template <int VEC> __device__ __forceinline__ void store_vec(float* __restrict__ p, const float* v)
@@ -192,25 +195,46 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_bwd(const TX* __restrict_
         for (int e = 0; e < VEC; ++e) dwa[c * VEC + e] = dba[c * VEC + e] = wv[c * VEC + e] = 0.f;
         if (col < d) load_vec<VEC>(w + col, wv + c * VEC);
     }
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR; row < m; row += (int64_t)gridDim.x * RPB) {
-        const bool live = !seg || seg[row] >= 0;
-        const float mean = stats[2 * row], rstd = stats[2 * row + 1];
+    // a row is loaded while the one before it is worked on
+    Raw<TX, VEC> rx[CPL];
+    Raw<TY, VEC> ry[CPL];
+    Raw<float, VEC> ra[CPL];
+    float mean = 0.f, rstd = 0.f;
+    bool live = false;
+    auto fetch = [&](int64_t row) {
+        live = !seg || seg[row] >= 0;
+        mean = stats[2 * row], rstd = stats[2 * row + 1];
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+            const int col = (c * LPR + lr) * VEC;
+            rx[c].clear(), ry[c].clear(), ra[c].clear();
+            if (col < d) {
+                rx[c].load(x + row * d + col);
+                ry[c].load(dy + row * d + col);
+                if (add) ra[c].load(add + row * d + col);
+            }
+        }
+    };
+    const int64_t first = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR;
+    if (first < m) fetch(first);
+    for (int64_t row = first; row < m; row += (int64_t)gridDim.x * RPB) {
+        const bool live_now = live;
+        const float mean_now = mean, rstd_now = rstd;
         float xh[CPL * VEC], g[CPL * VEC], ad[CPL * VEC];
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
-            const int col = (c * LPR + lr) * VEC;
+            const bool in = (c * LPR + lr) * VEC < d && live_now;      // padding is not used, whatever it holds
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) xh[c * VEC + e] = mean, g[c * VEC + e] = ad[c * VEC + e] = 0.f;
-            if (live && col < d) {
-                load_vec<VEC>(x + row * d + col, xh + c * VEC);
-                load_vec<VEC>(dy + row * d + col, g + c * VEC);
-                if (add) load_vec<VEC>(add + row * d + col, ad + c * VEC);
+            for (int e = 0; e < VEC; ++e) {
+                xh[c * VEC + e] = in ? (rx[c].get(e) - mean_now) * rstd_now : 0.f;
+                g[c * VEC + e] = in ? ry[c].get(e) : 0.f;
+                ad[c * VEC + e] = ra[c].get(e);
             }
         }
+        if (row + (int64_t)gridDim.x * RPB < m) fetch(row + (int64_t)gridDim.x * RPB);
 #pragma unroll
         for (int i = 0; i < CPL * VEC; ++i) {
-            xh[i] = live ? (xh[i] - mean) * rstd : 0.f;
             dwa[i] += g[i] * xh[i];
             dba[i] += g[i];
             g[i] *= wv[i];
@@ -227,7 +251,7 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_bwd(const TX* __restrict_
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const int i = c * VEC + e;
-                    o[e] = live ? rstd * (g[i] - mg - xh[i] * mgx) + ad[i] : 0.f;
+                    o[e] = live_now ? rstd_now * (g[i] - mg - xh[i] * mgx) + ad[i] : 0.f;
                 }
                 store_vec<VEC>(dx + row * d + col, o);
             }

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libgram.so")
@@ -111,7 +112,7 @@ def load():
     L.gram_unique_static.restype = C.c_int
     L.gram_unique_static.argtypes = [vp, C.c_int64, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp]
     i32, i64, f32 = C.c_int32, C.c_int64, C.c_float
-    acp, rp = C.POINTER(GramAttentionConfig), C.POINTER(GramRows)
+    acp, rp = C.POINTER(GramAttentionConfig), vp      # rp: the address of a GramRows
     L.gram_layer_norm.restype = C.c_int
     L.gram_layer_norm.argtypes = [vp, i32, vp, vp, vp, i64, i32, f32, vp, i32, vp, vp]
     L.gram_layer_norm_work_bytes.restype = i64
@@ -205,6 +206,8 @@ def unique_static(ids, vocab_n, pad_id, uniq, inverse, counts, u_dev, err_dev=No
 
 
 # ---- the collaborative filter's layer: calls without a context --------------------------------------------
+#
+# A small batch is bound by the host here, so the checks below are kept short: a call takes 5 to 10 us.
 
 
 def _ck_call(rc):
@@ -216,7 +219,13 @@ def _refuse(message):
     raise GramError(ERR_ARG, message)
 
 
-def _dtype_of(t, what):
+def _device():
+    """The current device's index, and -1 where there is none (host tensors are then refused like any other's)."""
+    import torch
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1
+
+
+def _elements(t, what):
     import torch
     if t.dtype is torch.bfloat16:
         return BF16
@@ -225,36 +234,34 @@ def _dtype_of(t, what):
     _refuse(f"{what}: float32 or bfloat16 expected, got {t.dtype}")
 
 
-def _flat(t, what, dtype, numel):
-    """Pointer of a contiguous tensor of that type and number of elements on the current device (None: NULL)."""
+def _flat(t, what, dtype, numel, dev):
+    """Pointer of a contiguous tensor of that type and number of elements on device `dev` (None: NULL)."""
     if t is None:
         return None
     if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
         _refuse(f"{what}: a contiguous {dtype} tensor of {numel} elements expected, got {t.dtype} {tuple(t.shape)}")
-    _here(t, what)
+    if not t.is_cuda or t.get_device() != dev:
+        _refuse(f"{what}: not on the current device")
     return t.data_ptr()
 
 
-def _here(t, what):
-    import torch
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
-        _refuse(f"{what}: not on the current device")
-
-
-def _bytes_of(work, what, size):
-    if work is None or work.numel() * work.element_size() < size or not work.is_contiguous():
+def _work(t, what, size, dev):
+    if t is None or t.numel() * t.element_size() < size or not t.is_contiguous():
         _refuse(f"{what}: a contiguous work buffer of at least {size} bytes expected")
-    _here(work, what)
-    return work.data_ptr()
+    if not t.is_cuda or t.get_device() != dev:
+        _refuse(f"{what}: not on the current device")
+    return t.data_ptr()
 
 
 def layer_norm_work_bytes(m, d):
     return int(load().gram_layer_norm_work_bytes(int(m), int(d)))
 
 
-def _norm_rows(x, what):
-    if x.dim() < 1 or not x.is_contiguous():
-        _refuse(f"{what}: contiguous rows expected")
+def _norm_rows(x, y, what, dev):
+    if x.dim() < 1 or y.shape != x.shape or not x.is_contiguous() or not y.is_contiguous():
+        _refuse(f"{what}: two contiguous tensors of one shape expected, got {tuple(x.shape)} and {tuple(y.shape)}")
+    if not x.is_cuda or x.get_device() != dev or not y.is_cuda or y.get_device() != dev:
+        _refuse(f"{what}: not on the current device")
     d = x.shape[-1]
     return (x.numel() // d if d else 0), d
 
@@ -264,35 +271,28 @@ def layer_norm(x, weight, bias, y, stats=None, segments=None, eps=1e-5, stream=N
     bfloat16, independently; stats ([rows, 2], float32) keeps mean and rstd for the backward pass; rows whose segment is
     negative are padding and become zero."""
     import torch
-    m, d = _norm_rows(x, "layer_norm: x")
-    f32 = torch.float32
-    if y.shape != x.shape or not y.is_contiguous():
-        _refuse("layer_norm: y must be contiguous, of x's shape")
-    _here(x, "layer_norm: x"), _here(y, "layer_norm: y")
-    _ck_call(load().gram_layer_norm(x.data_ptr(), _dtype_of(x, "layer_norm: x"), _flat(weight, "layer_norm: weight", f32, d),
-                                    _flat(bias, "layer_norm: bias", f32, d),
-                                    _flat(segments, "layer_norm: segments", torch.int32, m), m, d, eps, y.data_ptr(),
-                                    _dtype_of(y, "layer_norm: y"), _flat(stats, "layer_norm: stats", f32, 2 * m),
-                                    _stream(stream)))
+    L, dev, f32 = load(), _device(), torch.float32
+    m, d = _norm_rows(x, y, "layer_norm: x and y", dev)
+    _ck_call(L.gram_layer_norm(x.data_ptr(), _elements(x, "layer_norm: x"), _flat(weight, "layer_norm: weight", f32, d, dev),
+                               _flat(bias, "layer_norm: bias", f32, d, dev),
+                               _flat(segments, "layer_norm: segments", torch.int32, m, dev), m, d, eps, y.data_ptr(),
+                               _elements(y, "layer_norm: y"), _flat(stats, "layer_norm: stats", f32, 2 * m, dev),
+                               _stream(stream)))
 
 
 def layer_norm_backward(x, weight, stats, dy, dx, dweight, dbias, work, segments=None, add=None, stream=None):
     """gram_layer_norm_backward: dx (float32, plus `add` where given), dweight and dbias of layer_norm; work:
     layer_norm_work_bytes(rows, d) bytes."""
     import torch
-    what = "layer_norm_backward: "
-    m, d = _norm_rows(x, what + "x")
-    f32 = torch.float32
-    if dy.shape != x.shape or not dy.is_contiguous():
-        _refuse(what + "dy must be contiguous, of x's shape")
-    _here(x, what + "x"), _here(dy, what + "dy")
-    L = load()
-    _ck_call(L.gram_layer_norm_backward(x.data_ptr(), _dtype_of(x, what + "x"), _flat(weight, what + "weight", f32, d),
-                                        _flat(stats, what + "stats", f32, 2 * m), dy.data_ptr(), _dtype_of(dy, what + "dy"),
-                                        _flat(segments, what + "segments", torch.int32, m),
-                                        _flat(add, what + "add", f32, m * d), m, d, _flat(dx, what + "dx", f32, m * d),
-                                        _flat(dweight, what + "dweight", f32, d), _flat(dbias, what + "dbias", f32, d),
-                                        _bytes_of(work, what + "work", L.gram_layer_norm_work_bytes(m, d)), _stream(stream)))
+    what, L, dev, f32 = "layer_norm_backward: ", load(), _device(), torch.float32
+    m, d = _norm_rows(x, dy, what + "x and dy", dev)
+    _ck_call(L.gram_layer_norm_backward(
+        x.data_ptr(), _elements(x, what + "x"), _flat(weight, what + "weight", f32, d, dev),
+        _flat(stats, what + "stats", f32, 2 * m, dev), dy.data_ptr(), _elements(dy, what + "dy"),
+        _flat(segments, what + "segments", torch.int32, m, dev), _flat(add, what + "add", f32, m * d, dev), m, d,
+        _flat(dx, what + "dx", f32, m * d, dev), _flat(dweight, what + "dweight", f32, d, dev),
+        _flat(dbias, what + "dbias", f32, d, dev), _work(work, what + "work", L.gram_layer_norm_work_bytes(m, d), dev),
+        _stream(stream)))
 
 
 class HistoryAttention:
@@ -318,45 +318,40 @@ class HistoryAttention:
         """The bucket of the distance query position minus key position (-1 without a bias)."""
         return int(self._lib.gram_distance_bucket(self._cfg, int(distance)))
 
-    def _rows(self, t, what, batch, rows, heads):
-        st = t.stride()
-        if tuple(t.shape) != (batch, rows, heads, self.head_dim) or t.dtype is not self.dtype or \
-                (st[3] != 1 and self.head_dim != 1):
-            _refuse(f"{what}: {self.dtype} [{batch}, {rows}, {heads}, {self.head_dim}] with a contiguous last dimension "
-                    f"expected, got {t.dtype} {tuple(t.shape)}")
-        _here(t, what)
-        return C.byref(GramRows(t.data_ptr(), st[0], st[1], st[2]))
+    def _operands(self, call, dev, *named):
+        """gram_rows of the (name, tensor, shape) given, one after another; shapes of three dimensions have no rows."""
+        out = []
+        for name, t, shape in named:
+            if t.shape != shape or t.dtype is not self.dtype:
+                _refuse(f"{call}: {name}: {self.dtype} {list(shape)} expected, got {t.dtype} {list(t.shape)}")
+            st = t.stride()
+            if st[-1] != 1 and shape[-1] != 1:
+                _refuse(f"{call}: {name}: a contiguous last dimension expected, got strides {st}")
+            if not t.is_cuda or t.get_device() != dev:
+                _refuse(f"{call}: {name}: not on the current device")
+            out += (t.data_ptr(), st[0], st[1], st[2]) if len(st) == 4 else (t.data_ptr(), st[0], 0, st[1])
+        return array("q", out)
 
-    def _row(self, t, what, batch, heads):
-        st = t.stride()
-        if tuple(t.shape) != (batch, heads, self.head_dim) or t.dtype is not self.dtype or (st[2] != 1 and self.head_dim != 1):
-            _refuse(f"{what}: {self.dtype} [{batch}, {heads}, {self.head_dim}] with a contiguous last dimension expected, "
-                    f"got {t.dtype} {tuple(t.shape)}")
-        _here(t, what)
-        return C.byref(GramRows(t.data_ptr(), st[0], 0, st[1]))
-
-    def _table(self, t, what):
+    def _table(self, t, what, dev):
         import torch
         if (t is None) != (self.buckets == 0):
             _refuse(f"{what}: given exactly when the layer has buckets")
-        return _flat(t, what, torch.float32, self.heads * self.buckets)
-
-    def _sizes(self, q, what):
-        if q.dim() != 4:
-            _refuse(f"{what}: [batch, length, heads, head_dim] expected")
-        return q.shape[0], q.shape[1]
+        return _flat(t, what, torch.float32, self.heads * self.buckets, dev)
 
     def forward(self, q, k, v, o, lse=None, segments=None, prefix=None, table=None, stream=None):
         """o = attention of q over k, v.  lse ([batch, heads, length], float32) is kept for the backward pass; segments
         (int32 [batch, length], negative: padding) and prefix (int32 [batch]) mask; table ([heads, buckets], float32)."""
         import torch
-        B, L = self._sizes(q, "forward: q")
-        H, KV = self.heads, self.kv_heads
+        if q.dim() != 4:
+            _refuse("forward: q: [batch, length, heads, head_dim] expected")
+        B, L, dev = q.shape[0], q.shape[1], _device()
+        wide, shared = (B, L, self.heads, self.head_dim), (B, L, self.kv_heads, self.head_dim)
+        rows = self._operands("forward", dev, ("q", q, wide), ("k", k, shared), ("v", v, shared), ("o", o, wide))
+        at = rows.buffer_info()[0]
         _ck_call(self._lib.gram_attention(
-            self._cfg, B, L, self._rows(q, "forward: q", B, L, H), self._rows(k, "forward: k", B, L, KV),
-            self._rows(v, "forward: v", B, L, KV), self._rows(o, "forward: o", B, L, H),
-            _flat(segments, "forward: segments", torch.int32, B * L), _flat(prefix, "forward: prefix", torch.int32, B),
-            self._table(table, "forward: table"), _flat(lse, "forward: lse", torch.float32, B * H * L), _stream(stream)))
+            self._cfg, B, L, at, at + 32, at + 64, at + 96, _flat(segments, "forward: segments", torch.int32, B * L, dev),
+            _flat(prefix, "forward: prefix", torch.int32, B, dev), self._table(table, "forward: table", dev),
+            _flat(lse, "forward: lse", torch.float32, B * self.heads * L, dev), _stream(stream)))
 
     def backward_bytes(self, batch, length):
         return int(self._lib.gram_attention_backward_bytes(self._cfg, int(batch), int(length)))
@@ -366,19 +361,21 @@ class HistoryAttention:
         """dq, dk, dv and, where given, dtable from the gradient `do` of o, at the operands and outputs of forward; work:
         backward_bytes(batch, length) bytes."""
         import torch
-        B, L = self._sizes(q, "backward: q")
-        H, KV, i32, f32 = self.heads, self.kv_heads, torch.int32, torch.float32
-        rows = self._rows
+        if q.dim() != 4:
+            _refuse("backward: q: [batch, length, heads, head_dim] expected")
         if dtable is not None and self.buckets == 0:
             _refuse("backward: dtable without buckets")
+        B, L, dev, H, i32, f32 = q.shape[0], q.shape[1], _device(), self.heads, torch.int32, torch.float32
+        wide, shared = (B, L, H, self.head_dim), (B, L, self.kv_heads, self.head_dim)
+        rows = self._operands("backward", dev, ("q", q, wide), ("k", k, shared), ("v", v, shared), ("o", o, wide),
+                              ("do", do, wide), ("dq", dq, wide), ("dk", dk, shared), ("dv", dv, shared))
+        at = rows.buffer_info()[0]
         _ck_call(self._lib.gram_attention_backward(
-            self._cfg, B, L, rows(q, "backward: q", B, L, H), rows(k, "backward: k", B, L, KV),
-            rows(v, "backward: v", B, L, KV), rows(o, "backward: o", B, L, H), _flat(lse, "backward: lse", f32, B * H * L),
-            rows(do, "backward: do", B, L, H), rows(dq, "backward: dq", B, L, H), rows(dk, "backward: dk", B, L, KV),
-            rows(dv, "backward: dv", B, L, KV), _flat(segments, "backward: segments", i32, B * L),
-            _flat(prefix, "backward: prefix", i32, B), self._table(table, "backward: table"),
-            _flat(dtable, "backward: dtable", f32, H * self.buckets),
-            _bytes_of(work, "backward: work", self._lib.gram_attention_backward_bytes(self._cfg, B, L)), _stream(stream)))
+            self._cfg, B, L, at, at + 32, at + 64, at + 96, _flat(lse, "backward: lse", f32, B * H * L, dev), at + 128, at + 160,
+            at + 192, at + 224, _flat(segments, "backward: segments", i32, B * L, dev),
+            _flat(prefix, "backward: prefix", i32, B, dev), self._table(table, "backward: table", dev),
+            _flat(dtable, "backward: dtable", f32, H * self.buckets, dev),
+            _work(work, "backward: work", self._lib.gram_attention_backward_bytes(self._cfg, B, L), dev), _stream(stream)))
 
     def step_bytes(self, batch, capacity):
         return int(self._lib.gram_attention_step_bytes(self._cfg, int(batch), int(capacity)))
@@ -390,13 +387,15 @@ class HistoryAttention:
         import torch
         if q.dim() != 3 or k_cache.dim() != 4:
             _refuse("step: q [batch, heads, head_dim] and caches [batch, capacity, kv_heads, head_dim] expected")
-        B, cap, H, KV, i32 = q.shape[0], k_cache.shape[1], self.heads, self.kv_heads, torch.int32
+        B, rows_max, dev, KV, D = q.shape[0], k_cache.shape[1], _device(), self.kv_heads, self.head_dim
+        wide, new, cache = (B, self.heads, D), (B, KV, D), (B, rows_max, KV, D)
+        rows = self._operands("step", dev, ("q", q, wide), ("k_new", k_new, new), ("v_new", v_new, new),
+                              ("k_cache", k_cache, cache), ("v_cache", v_cache, cache), ("o", o, wide))
+        at = rows.buffer_info()[0]
         _ck_call(self._lib.gram_attention_step(
-            self._cfg, B, cap, self._row(q, "step: q", B, H), self._row(k_new, "step: k_new", B, KV),
-            self._row(v_new, "step: v_new", B, KV), self._rows(k_cache, "step: k_cache", B, cap, KV),
-            self._rows(v_cache, "step: v_cache", B, cap, KV), _flat(lengths, "step: lengths", i32, B),
-            _flat(first, "step: first", i32, B), self._table(table, "step: table"), self._row(o, "step: o", B, H),
-            _bytes_of(work, "step: work", self._lib.gram_attention_step_bytes(self._cfg, B, cap)), _stream(stream)))
+            self._cfg, B, rows_max, at, at + 32, at + 64, at + 96, at + 128, _flat(lengths, "step: lengths", torch.int32, B, dev),
+            _flat(first, "step: first", torch.int32, B, dev), self._table(table, "step: table", dev), at + 160,
+            _work(work, "step: work", self._lib.gram_attention_step_bytes(self._cfg, B, rows_max), dev), _stream(stream)))
 
 
 class Gram:
