@@ -13,7 +13,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libgram.so")
 SOURCES = ["gram_api.hip", "gram_sort.hip", "gram_stream.hip", "gram_gemm.hip", "gram_mlp.hip", "gram_norm.hip",
-           "gram_attend.hip", "gram_attend_fwd.hip", "gram_attend_dq.hip", "gram_attend_dkv.hip", "gram_attend_step.hip"]
+           "gram_attend.hip", "gram_attend_fwd.hip", "gram_attend_dq.hip", "gram_attend_dkv.hip",
+           "gram_attend_short.hip", "gram_attend_step.hip"]
 HEADERS = [os.path.join(CSRC, "gram_internal.h"), os.path.join(CSRC, "gram_mid_rows.h"),
            os.path.join(CSRC, "gram_attend.h"), os.path.join(ROOT, "include", "gram.h")]
 ARCH = "gfx950"

@@ -634,6 +634,71 @@ __device__ __forceinline__ void store_rows(unsigned char* room, const f32x4 (&ac
     __builtin_amdgcn_wave_barrier();
 }
 
+// ---- the gradient of the table ----------------------------------------------------------------------------
+
+constexpr int kNear = 383;       // distances that have a sum of their own
+constexpr int kStrip = 92;       // distances of a wave's 16 queries and a tile's 64 keys, each group's row of them
+
+// The table's gradient.  A tile of one bucket adds its ds to a register of each lane.  A tile of several adds along its
+// diagonals, which are the distances: lane (c, g) holds queries c and keys 16 n + 4 g + r, distance (a number of the tile)
+// + c - 4 g - r - 16 n.  Shifting the registers r = 1..3 by r lanes within their row of 16 brings equal distances
+// together; what is shifted out belongs to the same lanes' distances of n + 1.  That leaves five values a lane, distance
+// + c - 4 g - 16 n, n = 0..4; the four groups are joined through LDS, where the sum of a distance is added to the wave's
+// own `dist` row (distances within kNear) or, farther out where buckets are wide, bucket by bucket.  No word has two
+// writers, so every sum has one order.
+template <int SHIFT> __device__ __forceinline__ float row_shift(float v)        // lane i gets lane i + SHIFT's, 0 from outside
+{
+    constexpr int CTRL = SHIFT > 0 ? 0x100 | SHIFT : 0x110 | -SHIFT;            // row_shl, row_shr
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+
+__device__ __forceinline__ void add_bucket(float* bucket, int b, float lane_sums, int lane)
+{
+    const float sum = wave_total(lane_sums);
+    if (lane == 0) bucket[b] += sum;
+}
+
+// top: the distance of the wave's first query and the tile's first key.
+__device__ __forceinline__ void table_near(const AttArgs& a, const f32x4 (&ds)[4], int top, float (*strip)[kStrip], float* dist,
+                                           float* bucket, const int* border, int lane)
+{
+    const int c = lane & 15, g = lane >> 4;
+    float spill = 0.f;
+    // distance top + c - 4 g - 16 n lies at place c - 4 g - 16 n + 76 of its group's row
+    float* const at = &strip[g][c - 4 * g + 76];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        at[-16 * n] = ds[n][0] + row_shift<1>(ds[n][1]) + row_shift<2>(ds[n][2]) + row_shift<3>(ds[n][3]) + spill;
+        spill = row_shift<-15>(ds[n][1]) + row_shift<-14>(ds[n][2]) + row_shift<-13>(ds[n][3]);
+    }
+    at[-64] = spill;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    float sum[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int place = lane + 64 * h;
+        sum[h] = 0.f;
+        if (place < kStrip) sum[h] = (strip[0][place] + strip[1][place]) + (strip[2][place] + strip[3][place]);
+    }
+    __builtin_amdgcn_wave_barrier();
+    const int n0 = top - 76;                                   // distance of place 0
+    if (n0 >= -kNear && n0 + kStrip - 1 <= kNear) {
+        dist[n0 + lane] += sum[0];
+        if (lane + 64 < kStrip) dist[n0 + 64 + lane] += sum[1];
+    } else {
+        const int b0 = bucket_of(a.bk, border, n0 + lane), b1 = bucket_of(a.bk, border, n0 + 64 + lane);
+        uint64_t left0 = ~0ull, left1 = __ballot(lane + 64 < kStrip);
+        while (left0 | left1) {
+            const int b = left0 ? __builtin_amdgcn_readlane(b0, __builtin_ctzll(left0)) : __builtin_amdgcn_readlane(b1, __builtin_ctzll(left1));
+            const bool m0 = b0 == b, m1 = lane + 64 < kStrip && b1 == b;
+            add_bucket(bucket, b, (m0 ? sum[0] : 0.f) + (m1 ? sum[1] : 0.f), lane);
+            left0 &= ~__ballot(m0), left1 &= ~__ballot(m1);
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // ---- launches ---------------------------------------------------------------------------------------------
 // unit: bytes per global access (template argument UNIT): 16, 8 (bf16 only), or the size of an element
 template <typename F> inline void by_shape(const gram_attention_config& c, int unit, F&& go)
@@ -663,6 +728,8 @@ inline dim3 att_grid(int items) { return dim3((unsigned)((items + 7) / 8 * 8)); 
 constexpr int att_blocks(int length, int rows) { return (length + rows - 1) / rows; }
 
 void attend_forward(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s);      // gram_attend_fwd.hip
+// Histories of one tile: all gradients in one launch.  False: not for this shape.
+bool attend_backward_short(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s);       // gram_attend_short.hip
 void attend_backward_queries(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s);     // gram_attend_dq.hip
 void attend_backward_keys(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s);        // gram_attend_dkv.hip
 

@@ -1,5 +1,5 @@
 // Attention over item histories: the C entry points, their checks, and the last sum of the table's gradient.  The kernels
-// are in gram_attend_fwd.hip, gram_attend_dq.hip, gram_attend_dkv.hip and gram_attend_step.hip.
+// are in gram_attend_fwd.hip, gram_attend_dq.hip, gram_attend_dkv.hip, gram_attend_short.hip and gram_attend_step.hip.
 #include <math.h>
 
 #include "gram_attend.h"
@@ -204,8 +204,10 @@ int gram_attention_backward(const gram_attention_config* cfg, int32_t batch, int
                         : nullptr;
         a.parts = batch * att_blocks(length, kTile);
         const int unit = u.unit(cfg->head_dim, es);
-        attend_backward_queries(*cfg, a, unit, s);      // also leaves delta for the pass over the keys
-        attend_backward_keys(*cfg, a, unit, s);
+        if (!attend_backward_short(*cfg, a, unit, s)) {
+            attend_backward_queries(*cfg, a, unit, s);  // also leaves delta for the pass over the keys
+            attend_backward_keys(*cfg, a, unit, s);
+        }
     }
     if (dtable)
         k_attend_dtable<<<dim3((unsigned)((cfg->buckets + 15) / 16), (unsigned)cfg->heads), dim3(1024), 0, s>>>(

@@ -13,8 +13,6 @@ namespace gram {
 
 namespace {
 
-constexpr int kNear = 383;       // distances that have a sum of their own
-constexpr int kStrip = 92;       // distances of a wave's 16 queries and a tile's 64 keys, each group's row of them
 
 template <typename T, int DP> struct DqShared {
     __attribute__((aligned(1024))) unsigned char k[Shape<T, DP>::TILE], v[Shape<T, DP>::TILE];
@@ -26,66 +24,6 @@ template <typename T, int DP> struct DqShared {
     float bucket[kWavesPerBlock][kMaxBorders];     // sums of ds by bucket, each wave's own
     TileMarks marks;
 };
-
-// The table's gradient.  A tile of one bucket adds its ds to a register of each lane.  A tile of several adds along its
-// diagonals, which are the distances: lane (c, g) holds queries c and keys 16 n + 4 g + r, distance (a number of the tile)
-// + c - 4 g - r - 16 n.  Shifting the registers r = 1..3 by r lanes within their row of 16 brings equal distances
-// together; what is shifted out belongs to the same lanes' distances of n + 1.  That leaves five values a lane, distance
-// + c - 4 g - 16 n, n = 0..4; the four groups are joined through LDS, where the sum of a distance is added to the wave's
-// own `dist` row (distances within kNear) or, farther out where buckets are wide, bucket by bucket.  No word has two
-// writers, so every sum has one order.
-template <int SHIFT> __device__ __forceinline__ float row_shift(float v)        // lane i gets lane i + SHIFT's, 0 from outside
-{
-    constexpr int CTRL = SHIFT > 0 ? 0x100 | SHIFT : 0x110 | -SHIFT;            // row_shl, row_shr
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
-}
-
-__device__ __forceinline__ void add_bucket(float* bucket, int b, float lane_sums, int lane)
-{
-    const float sum = wave_total(lane_sums);
-    if (lane == 0) bucket[b] += sum;
-}
-
-// top: the distance of the wave's first query and the tile's first key.
-__device__ __forceinline__ void table_near(const AttArgs& a, const f32x4 (&ds)[4], int top, float (*strip)[kStrip], float* dist,
-                                           float* bucket, const int* border, int lane)
-{
-    const int c = lane & 15, g = lane >> 4;
-    float spill = 0.f;
-    // distance top + c - 4 g - 16 n lies at place c - 4 g - 16 n + 76 of its group's row
-    float* const at = &strip[g][c - 4 * g + 76];
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        at[-16 * n] = ds[n][0] + row_shift<1>(ds[n][1]) + row_shift<2>(ds[n][2]) + row_shift<3>(ds[n][3]) + spill;
-        spill = row_shift<-15>(ds[n][1]) + row_shift<-14>(ds[n][2]) + row_shift<-13>(ds[n][3]);
-    }
-    at[-64] = spill;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    float sum[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int place = lane + 64 * h;
-        sum[h] = 0.f;
-        if (place < kStrip) sum[h] = (strip[0][place] + strip[1][place]) + (strip[2][place] + strip[3][place]);
-    }
-    __builtin_amdgcn_wave_barrier();
-    const int n0 = top - 76;                                   // distance of place 0
-    if (n0 >= -kNear && n0 + kStrip - 1 <= kNear) {
-        dist[n0 + lane] += sum[0];
-        if (lane + 64 < kStrip) dist[n0 + 64 + lane] += sum[1];
-    } else {
-        const int b0 = bucket_of(a.bk, border, n0 + lane), b1 = bucket_of(a.bk, border, n0 + 64 + lane);
-        uint64_t left0 = ~0ull, left1 = __ballot(lane + 64 < kStrip);
-        while (left0 | left1) {
-            const int b = left0 ? __builtin_amdgcn_readlane(b0, __builtin_ctzll(left0)) : __builtin_amdgcn_readlane(b1, __builtin_ctzll(left1));
-            const bool m0 = b0 == b, m1 = lane + 64 < kStrip && b1 == b;
-            add_bucket(bucket, b, (m0 ? sum[0] : 0.f) + (m1 ? sum[1] : 0.f), lane);
-            left0 &= ~__ballot(m0), left1 &= ~__ballot(m1);
-        }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-}
 
 // One block: 64 queries of one head.  Dynamic LDS: kWavesPerBlock rows of 2 kNear + 1 sums of ds by distance.
 template <typename T, int DP, int UNIT, bool CAP, int WAVES>

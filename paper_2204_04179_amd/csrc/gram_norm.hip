@@ -287,20 +287,26 @@ __global__ __launch_bounds__(kBlock) void k_layer_norm_bwd(const TX* __restrict_
     }
 }
 
-// dw and db from the partial rows: 16 columns per block, 16 strands of rows each, added in a fixed order.
-__global__ __launch_bounds__(kBlock) void k_layer_norm_parts(const float* __restrict__ part, int parts, int d,
-                                                             float* __restrict__ dw, float* __restrict__ db)
+// dw and db from the partial rows: 16 columns per block, 64 strands of rows each, added in a fixed order.
+__global__ __launch_bounds__(1024) void k_layer_norm_parts(const float* __restrict__ part, int parts, int d,
+                                                           float* __restrict__ dw, float* __restrict__ db)
 {
-    __shared__ float s[kBlock];
+    __shared__ float s[1024];
     const int col = blockIdx.x * 16 + threadIdx.x % 16, strand = threadIdx.x / 16;
     float sum = 0.f;
-    if (col < 2 * d)
-        for (int p = strand; p < parts; p += 16) sum += part[(int64_t)p * 2 * d + col];
+    if (col < 2 * d) {
+        const float* const p = part + col;
+#pragma unroll 8
+        for (int i = strand; i < parts; i += 64) sum += p[(int64_t)i * 2 * d];
+    }
     s[threadIdx.x] = sum;
     __syncthreads();
+    if (threadIdx.x < 256) s[threadIdx.x] = (s[threadIdx.x] + s[threadIdx.x + 256]) + (s[threadIdx.x + 512] + s[threadIdx.x + 768]);
+    __syncthreads();
     if (strand == 0 && col < 2 * d) {
+        sum = 0.f;
 #pragma unroll
-        for (int t = 1; t < 16; ++t) sum += s[t * 16 + threadIdx.x];
+        for (int t = 0; t < 16; ++t) sum += s[t * 16 + threadIdx.x];
         if (col < d) dw[col] = sum;
         else db[col - d] = sum;
     }
@@ -421,7 +427,7 @@ int gram_layer_norm_backward(const void* x, int32_t x_dtype, const float* weight
             });
         });
     }
-    k_layer_norm_parts<<<dim3((unsigned)((2 * d + 15) / 16)), dim3(kBlock), 0, s>>>(part, parts, d, dweight, dbias);
+    k_layer_norm_parts<<<dim3((unsigned)((2 * d + 15) / 16)), dim3(1024), 0, s>>>(part, parts, d, dweight, dbias);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? GRAM_OK : fail_call(GRAM_ERR_HIP, "gram_layer_norm_backward: %s", hipGetErrorString(e));
 }
