@@ -31,6 +31,19 @@ typedef s16x4 __attribute__((address_space(3))) lds_s16x4;
 
 struct Bf16 { uint16_t bits; };
 
+// Division of work items by a number of the launch: floor(n / d) = (n * mul) >> (32 + shift) for n below 2^31, with mul =
+// ceil(2^(32 + shift) / d), shift = ceil(log2 d) - 1 (d = 1: no multiplication).
+struct FastDiv {
+    uint32_t d, mul, shift;
+    __host__ static FastDiv of(uint32_t d)
+    {
+        uint32_t s = 0;
+        while ((1u << (s + 1)) < d && s < 30) ++s;
+        return {d, d == 1 ? 0u : (uint32_t)((((uint64_t)1 << (32 + s)) + d - 1) / d), s};
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return d == 1 ? n : __umulhi(n, mul) >> shift; }
+};
+
 // One operand: element (b, row, head, 0) is at data + b * sb + row * sr + head * sh.
 struct AttRows {
     void* data;
@@ -59,6 +72,7 @@ struct AttArgs {
     int batch, length, heads, kv_heads, group, dim;
     int causal;
     int items, parts;
+    FastDiv by_tiles, by_heads, by_group;      // tiles of a history; heads or key heads; heads that share a key head
     float scale, cap;
     AttBuckets bk;
 };
@@ -507,7 +521,8 @@ template <typename T, int DP, int UNIT> struct Feed {
     int seg;                                          // of row (lane) of the tile
 
     __device__ __forceinline__ explicit Feed(int thread) : tid(thread), seg(kNoSeg) {}
-    // pa, pb: row row0 of the operands
+    // pa, pb: row row0 of the operands; BOTH false: a alone
+    template <bool BOTH = true>
     __device__ __forceinline__ void load(const T* pa, int64_t sa, const T* pb, int64_t sb, int row0, int length,
                                          const int* __restrict__ segments, int dim)
     {
@@ -517,13 +532,14 @@ template <typename T, int DP, int UNIT> struct Feed {
 #pragma unroll
         for (int i = 0; i < S::NC; ++i) {
             a[i] = load_chunk<T, UNIT>(ra, (row + i * STEP) * ra.stride, ch, dim);
-            b[i] = load_chunk<T, UNIT>(rb, (row + i * STEP) * rb.stride, ch, dim);
+            if constexpr (BOTH) b[i] = load_chunk<T, UNIT>(rb, (row + i * STEP) * rb.stride, ch, dim);
+            else b[i] = u32x4{0u, 0u, 0u, 0u};
         }
         seg = row_segment(segments, row0 + (tid & (kWave - 1)), length);
     }
     // masked: the tile has masked pairs.  MARK_A: the mark of a row is a NaN among its elements of a (the operand of the first
     // product only); else its bit in bad[].
-    template <bool MARK_A>
+    template <bool MARK_A, bool BOTH = true>
     __device__ __forceinline__ void put(unsigned char* ta, unsigned char* tb, int* s_seg, bool masked, uint32_t* bad)
     {
         const int row = (uint32_t)tid / S::NCH, ch = (uint32_t)tid % S::NCH;
@@ -550,7 +566,7 @@ template <typename T, int DP, int UNIT> struct Feed {
         for (int i = 0; i < S::NC; ++i) {
             const int at = (row + i * STEP) * S::RB + ((ch ^ swz<T, S::NCH>(row + i * STEP)) * 16);
             *reinterpret_cast<u32x4*>(ta + at) = a[i];
-            *reinterpret_cast<u32x4*>(tb + at) = b[i];
+            if constexpr (BOTH) *reinterpret_cast<u32x4*>(tb + at) = b[i];
         }
     }
 };

@@ -39,8 +39,9 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dkv(const AttArgs a)
     if (item < 0) return;
     const int tid = threadIdx.x, lane = lane_id();
     const int ntiles = (a.length + kTile - 1) / kTile;
-    const int kt = item % ntiles;
-    const int kvh = (item / ntiles) % a.kv_heads, batch = item / ntiles / a.kv_heads;
+    const int rows_item = (int)a.by_tiles.quotient((uint32_t)item);       // history and key head
+    const int kt = item - rows_item * ntiles;
+    const int batch = (int)a.by_heads.quotient((uint32_t)rows_item), kvh = rows_item - batch * a.kv_heads;
     const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int k0 = kt * kTile, wk0 = k0 + wave * 16, k = wk0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
@@ -159,6 +160,7 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dkv(const AttArgs a)
 void attend_backward_keys(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s)
 {
     a.items = a.batch * a.kv_heads * att_blocks(a.length, kTile);
+    a.by_tiles = FastDiv::of(att_blocks(a.length, kTile)), a.by_heads = FastDiv::of(a.kv_heads);
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
         constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 3 : 2;

@@ -26,19 +26,23 @@ template <typename T, int DP> struct DqShared {
 };
 
 // One block: 64 queries of one head.  Dynamic LDS: kWavesPerBlock rows of 2 kNear + 1 sums of ds by distance.
-template <typename T, int DP, int UNIT, bool CAP, int WAVES>
+// KEEP > 0: histories of at most KEEP tiles; weights and products of the first walk stay in registers, and the second walk
+// loads the keys alone (queries of 1024 x 200, 8 heads of 128: 1.43 ms without).
+template <typename T, int DP, int UNIT, bool CAP, int WAVES, int KEEP>
 __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
 {
     using S = Shape<T, DP>;
-    constexpr bool AHEAD = S::RB < 256;
+    constexpr bool AHEAD = S::RB < 256 && KEEP == 0;
     extern __shared__ float dist[];
     __shared__ DqShared<T, DP> sh;
     const int item = xcd_item(a.items);
     if (item < 0) return;
     const int tid = threadIdx.x, lane = lane_id();
     const int nqt = (a.length + kTile - 1) / kTile;
-    const int qt = nqt - 1 - item % nqt;
-    const int head = (item / nqt) % a.heads, batch = item / nqt / a.heads, kvh = head / a.group;
+    const int rows_item = (int)a.by_tiles.quotient((uint32_t)item);       // history and head
+    const int qt = nqt - 1 - (item - rows_item * nqt);
+    const int batch = (int)a.by_heads.quotient((uint32_t)rows_item), head = rows_item - batch * a.heads;
+    const int kvh = (int)a.by_group.quotient((uint32_t)head);
     const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int q0 = qt * kTile, wq0 = q0 + wave * 16, q = wq0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
@@ -120,6 +124,57 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
             for (int w = 0; w < kWavesPerBlock; ++w) sh.bucket[w][tid] = 0.f;
         delta = 0.f;
     }
+    // a tile's keys and values (or keys alone) to LDS
+    auto flat_of = [&](int t) {
+        const int hi = q0 + kTile - 1 - t * kTile;
+        return a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
+    };
+    auto sees = [&](int t) { return wq0 < a.length && !(a.causal && t * kTile > wq0 + 15 && t * kTile >= prefix); };
+    // weights and dp of a tile in LDS
+    auto weigh = [&](int t, bool mixed, f32x4 (&s)[4], f32x4 (&dp)[4], f32x4 (&slope)[CAP ? 4 : 1]) {
+        const int k0 = t * kTile, flat = flat_of(t);
+        first_product<T, DP>(s, qf, rd, sh.k);
+        to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? sh.table[flat] : 0.f);
+        if (flat < 0) add_bias(s, &sh.bias[4 * g - (q - q0) + kTile - 1]);
+        if (!whole(t, wq0, mixed) || !full_rows) {
+            if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0, lane);
+            else mask_scores<false, false>(s, sh.seg, own, last - k0, lane);
+        }
+        first_product<T, DP>(dp, df, rd, sh.v);
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - lse2);
+    };
+    auto add_delta = [&](const f32x4 (&s)[4], const f32x4 (&dp)[4]) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) delta += s[n][r] * dp[n][r];
+    };
+    // ds in place of the weights, and what they add to the table's gradient
+    auto table_sums = [&](int t, f32x4 (&s)[4], const f32x4 (&dp)[4]) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[n][r] *= dp[n][r] - delta;
+        if (!want_table) return;
+        const int flat = flat_of(t);
+        if (flat >= 0) {
+            if (flat != flat_bucket) {
+                if (flat_bucket >= 0) add_bucket(sh.bucket[wave], flat_bucket, flat_sum, lane);
+                flat_bucket = flat, flat_sum = 0.f;
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) flat_sum += (s[n][0] + s[n][1]) + (s[n][2] + s[n][3]);
+        } else {
+            table_near(a, s, wq0 - t * kTile, sh.strip[wave], my_dist, sh.bucket[wave], sh.border, lane);
+        }
+    };
+    auto put_bias = [&](int t) {
+        const int hi = q0 + kTile - 1 - t * kTile;
+        if (flat_of(t) < 0 && tid < 2 * kTile - 1) sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, hi - tid)];
+    };
     // DELTA: only sum p dp; else the gradients, with that sum on the way where the one tile holds it all
     auto walk = [&](auto delta_only) {
         constexpr bool DELTA = decltype(delta_only)::value;
@@ -127,55 +182,20 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
         if (AHEAD && t < t1) load(t);
         while (t < t1) {
             const bool mixed = tile_mixed(mk, t);
-            const int k0 = t * kTile, hi = q0 + kTile - 1 - k0;
-            const int flat = a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
             if (!AHEAD) load(t);
             __syncthreads();
             feed.template put<false>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
-            if (flat < 0 && tid < 2 * kTile - 1)
-                sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, hi - tid)];
+            put_bias(t);
             const int tn = next_tile(t + 1, t1, mk);
             if (AHEAD && tn < t1) load(tn);
             __syncthreads();
-            const bool sees = wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix);
-            if (sees) {
+            if (sees(t)) {
                 f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
-                first_product<T, DP>(s, qf, rd, sh.k);
-                to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? sh.table[flat] : 0.f);
-                if (flat < 0) add_bias(s, &sh.bias[4 * g - (q - q0) + kTile - 1]);
-                if (!whole(t, wq0, mixed) || !full_rows) {
-                    if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0, lane);
-                    else mask_scores<false, false>(s, sh.seg, own, last - k0, lane);
-                }
-                first_product<T, DP>(dp, df, rd, sh.v);
-#pragma unroll
-                for (int n = 0; n < 4; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - lse2);
-                if (DELTA || (want_table && one_tile)) {
-#pragma unroll
-                    for (int n = 0; n < 4; ++n)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) delta += s[n][r] * dp[n][r];
-                }
+                weigh(t, mixed, s, dp, slope);
+                if (DELTA || (want_table && one_tile)) add_delta(s, dp);
                 if constexpr (!DELTA) {
                     if (want_table && one_tile) delta = group_sum(delta);
-#pragma unroll
-                    for (int n = 0; n < 4; ++n)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[n][r] *= dp[n][r] - delta;
-                    if (want_table) {
-                        if (flat >= 0) {
-                            if (flat != flat_bucket) {
-                                if (flat_bucket >= 0) add_bucket(sh.bucket[wave], flat_bucket, flat_sum, lane);
-                                flat_bucket = flat, flat_sum = 0.f;
-                            }
-#pragma unroll
-                            for (int n = 0; n < 4; ++n) flat_sum += (s[n][0] + s[n][1]) + (s[n][2] + s[n][3]);
-                        } else {
-                            table_near(a, s, wq0 - k0, sh.strip[wave], my_dist, sh.bucket[wave], sh.border, lane);
-                        }
-                    }
+                    table_sums(t, s, dp);
                     if constexpr (CAP) {
 #pragma unroll
                         for (int n = 0; n < 4; ++n) s[n] *= slope[n];
@@ -187,8 +207,49 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
         }
         if constexpr (DELTA) delta = group_sum(delta);
     };
-    if (want_table && !one_tile) walk(std::true_type{});
-    walk(std::false_type{});
+    if constexpr (KEEP > 0) {
+        f32x4 s[KEEP][4], dp[KEEP][4], none[1];
+        int tile[KEEP];
+        int t = tfirst;
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+            tile[i] = t;
+            if (t < t1) {
+                const bool mixed = tile_mixed(mk, t);
+                load(t);
+                __syncthreads();
+                feed.template put<false>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
+                put_bias(t);
+                __syncthreads();
+                if (sees(t)) {
+                    weigh(t, mixed, s[i], dp[i], none);
+                    add_delta(s[i], dp[i]);
+                }
+                t = next_tile(t + 1, t1, mk);
+            }
+        }
+        delta = group_sum(delta);
+        bool there = true;                           // the keys of the last tile are in LDS still
+#pragma unroll
+        for (int i = KEEP - 1; i >= 0; --i) {
+            if (tile[i] >= t1) continue;
+            if (!there) {
+                const int k0 = tile[i] * kTile;
+                feed.template load<false>(kp + k0 * a.k.sr, a.k.sr, kp, a.k.sr, k0, a.length, seg, a.dim);
+                __syncthreads();
+                feed.template put<false, false>(sh.k, sh.v, sh.seg, !whole(tile[i], q0, tile_mixed(mk, tile[i])), nullptr);
+                __syncthreads();
+            }
+            there = false;
+            if (sees(tile[i])) {
+                table_sums(tile[i], s[i], dp[i]);
+                second_product<T, DP>(dq, s[i], rd, sh.k);
+            }
+        }
+    } else {
+        if (want_table && !one_tile) walk(std::true_type{});
+        walk(std::false_type{});
+    }
     __syncthreads();
     if (wq0 < a.length) {
         T* const dqp = static_cast<T*>(a.dq.data) + batch * a.dq.sb + head * a.dq.sh + wq0 * a.dq.sr;
@@ -226,11 +287,24 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
 void attend_backward_queries(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s)
 {
     a.items = a.batch * a.heads * att_blocks(a.length, kTile);
+    a.by_tiles = FastDiv::of(att_blocks(a.length, kTile)), a.by_heads = FastDiv::of(a.heads), a.by_group = FastDiv::of(a.group);
     const size_t dist = a.part ? kWavesPerBlock * (2 * kNear + 1) * sizeof(float) : 0;
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
         constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 3 : 2;
-        k_attend_dq<decltype(type), DP, decltype(u)::value, decltype(cap)::value, WAVES><<<att_grid(a.items), dim3(kBlock), dist, s>>>(a);
+        auto go = [&](auto keep) {
+            constexpr int KEEP = decltype(keep)::value;
+            k_attend_dq<decltype(type), DP, decltype(u)::value, decltype(cap)::value, (KEEP > 2 ? 2 : WAVES), KEEP>
+                <<<att_grid(a.items), dim3(kBlock), dist, s>>>(a);
+        };
+        // kept are the tiles of histories of up to 256 positions, where there are two walks, no slopes to keep as well, and
+        // registers for it all: rows of 512 bytes leave none
+        if constexpr (!decltype(cap)::value && Shape<decltype(type), DP>::RB <= 256) {
+            const int tiles = att_blocks(a.length, kTile);
+            if (a.part && tiles == 2) return go(std::integral_constant<int, 2>{});
+            if (a.part && (tiles == 3 || tiles == 4)) return go(std::integral_constant<int, 4>{});
+        }
+        go(std::integral_constant<int, 0>{});
     });
 }
 

@@ -31,8 +31,10 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend(const AttArgs a)
     if (item < 0) return;
     const int tid = threadIdx.x, lane = lane_id();
     const int nqt = (a.length + kTile - 1) / kTile;
-    const int qt = nqt - 1 - item % nqt;                 // the longest rows of a causal mask first
-    const int head = (item / nqt) % a.heads, batch = item / nqt / a.heads, kvh = head / a.group;
+    const int rows_item = (int)a.by_tiles.quotient((uint32_t)item);       // history and head
+    const int qt = nqt - 1 - (item - rows_item * nqt);                 // the longest rows of a causal mask first
+    const int batch = (int)a.by_heads.quotient((uint32_t)rows_item), head = rows_item - batch * a.heads;
+    const int kvh = (int)a.by_group.quotient((uint32_t)head);
     const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int q0 = qt * kTile, wq0 = q0 + wave * 16, q = wq0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
@@ -144,6 +146,7 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend(const AttArgs a)
 void attend_forward(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s)
 {
     a.items = a.batch * a.heads * att_blocks(a.length, kTile);
+    a.by_tiles = FastDiv::of(att_blocks(a.length, kTile)), a.by_heads = FastDiv::of(a.heads), a.by_group = FastDiv::of(a.group);
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
         // blocks per CU that registers allow: accumulators, fragments and the tile under way grow with the row's bytes

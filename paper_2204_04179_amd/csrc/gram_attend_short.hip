@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_a
     const int item = xcd_item(a.items);
     if (item < 0) return;
     const int tid = threadIdx.x, lane = lane_id();
-    const int kvh = item % a.kv_heads, batch = item / a.kv_heads;
+    const int batch = (int)a.by_heads.quotient((uint32_t)item), kvh = item - batch * a.kv_heads;
     const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int w0 = wave * 16, row = w0 + c;                     // the wave's rows, as queries and as keys
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
@@ -93,6 +93,15 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_a
     Feed<T, DP, UNIT> feed(tid);
     feed.load(static_cast<const T*>(a.k.data) + batch * a.k.sb + kvh * a.k.sh, a.k.sr,
               static_cast<const T*>(a.v.data) + batch * a.v.sb + kvh * a.v.sh, a.v.sr, 0, a.length, seg, a.dim);
+    Feed<T, DP, UNIT> queries(tid);                             // of the first head, on their way with the keys
+    float lse_ahead = 0.f;
+    auto load_queries = [&](int h) {
+        const int head = kvh * a.group + h;
+        queries.load(static_cast<const T*>(a.q.data) + batch * a.q.sb + head * a.q.sh, a.q.sr,
+                     static_cast<const T*>(a.dout.data) + batch * a.dout.sb + head * a.dout.sh, a.dout.sr, 0, a.length, seg, a.dim);
+        lse_ahead = a.lse[((int64_t)batch * a.heads + head) * a.length + (row < a.length ? row : a.length - 1)];
+    };
+    load_queries(0);
     feed.template put<false>(sh.k, sh.v, sh.seg, masked, nullptr);
 
     const Reader<T, DP> rd(lane);
@@ -104,12 +113,10 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_a
 
     for (int h = 0; h < a.group; ++h) {
         const int head = kvh * a.group + h;
-        feed.load(static_cast<const T*>(a.q.data) + batch * a.q.sb + head * a.q.sh, a.q.sr,
-                  static_cast<const T*>(a.dout.data) + batch * a.dout.sb + head * a.dout.sh, a.dout.sr, 0, a.length, seg, a.dim);
-        const float lse = a.lse[((int64_t)batch * a.heads + head) * a.length + (row < a.length ? row : a.length - 1)];
+        const float lse = lse_ahead;
         if (tid < buckets) sh.table[tid] = a.table[(int64_t)head * buckets + tid] * kLog2e;
         __syncthreads();                                        // the last head's tiles have been read; table and bad are set
-        feed.template put<false>(sh.q, sh.d, sh.seg, masked, sh.bad);
+        queries.template put<false>(sh.q, sh.d, sh.seg, masked, sh.bad);
         if (flat < 0 && tid < 2 * kTile - 1) sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, kTile - 1 - tid)];
         if (want_table) {
             for (int i = tid; i < kWavesPerBlock * (2 * kShortDist + 1); i += kBlock) (&sh.dist[0][0])[i] = 0.f;
@@ -192,6 +199,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_a
                 if (sub == 0) a.part[((int64_t)head * a.parts + batch) * buckets + b] = sum;
             }
         }
+        if (h + 1 < a.group) load_queries(h + 1);
         __syncthreads();                                        // the tiles have been read
         if (tid < 2) sh.bad[tid] = 0u;
         if (w0 < a.length) {
@@ -215,6 +223,7 @@ bool attend_backward_short(const gram_attention_config& c, AttArgs a, int unit, 
     // four tiles of rows and two of weights have to fit a CU's LDS: float32 rows of more than 64 elements do not
     if (a.length > kTile || (c.dtype == GRAM_F32 && c.head_dim > 64)) return false;
     a.items = a.batch * a.kv_heads;
+    a.by_heads = FastDiv::of(a.kv_heads);
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         using T = decltype(type);
         constexpr int DP = decltype(dp)::value;
