@@ -219,11 +219,12 @@ template <typename T, int DP> struct Reader {
     }
 };
 
-// acc[dt] += (streamed tile transposed) . w, the w of a first product's layout.  Fragments are read one group ahead of the
-// products that take them; the barriers keep the compiler from reading all of them at once, for want of registers.
-template <typename T, int DP>
-__device__ __forceinline__ void second_product(f32x4 (&acc)[DP / 16], const f32x4 (&w)[4], const Reader<T, DP>& rd,
-                                               const unsigned char* tile)
+// acc[m][dt] += (streamed tile transposed) . w[m], the w of a first product's layout, for M sets of weights that share the
+// tile.  Fragments are read one group ahead of the products that take them; the barriers keep the compiler from reading all
+// of them at once, for want of registers.
+template <typename T, int DP, int M>
+__device__ __forceinline__ void second_products(f32x4 (&acc)[M][DP / 16], const f32x4 (&w)[M][4], const Reader<T, DP>& rd,
+                                                const unsigned char* tile)
 {
     using S = Shape<T, DP>;
     constexpr int STEPS = sizeof(T) == 2 ? 2 : 4;              // pieces of the 64 rows
@@ -241,16 +242,26 @@ __device__ __forceinline__ void second_product(f32x4 (&acc)[DP / 16], const f32x
     for (int n = 0; n < N; ++n) {
         if (n + 1 < N) read(n + 1, f[(n + 1) & 1]);
         const int step = n / PER;
-        u32x4 b;
-        if constexpr (sizeof(T) == 2)       // rounded to nearest even, to as many bits as the other operand has
-            b = u32x4{pack_bf16x2(w[2 * step][0], w[2 * step][1]), pack_bf16x2(w[2 * step][2], w[2 * step][3]),
-                      pack_bf16x2(w[2 * step + 1][0], w[2 * step + 1][1]), pack_bf16x2(w[2 * step + 1][2], w[2 * step + 1][3])};
-        else
-            b = __builtin_bit_cast(u32x4, w[step]);
 #pragma unroll
-        for (int i = 0; i < G; ++i) acc[(n % PER) * G + i] = mma<T>(f[n & 1][i], b, acc[(n % PER) * G + i]);
+        for (int m = 0; m < M; ++m) {
+            u32x4 b;
+            if constexpr (sizeof(T) == 2)   // rounded to nearest even, to as many bits as the other operand has
+                b = u32x4{pack_bf16x2(w[m][2 * step][0], w[m][2 * step][1]), pack_bf16x2(w[m][2 * step][2], w[m][2 * step][3]),
+                          pack_bf16x2(w[m][2 * step + 1][0], w[m][2 * step + 1][1]),
+                          pack_bf16x2(w[m][2 * step + 1][2], w[m][2 * step + 1][3])};
+            else
+                b = __builtin_bit_cast(u32x4, w[m][step]);
+#pragma unroll
+            for (int i = 0; i < G; ++i) acc[m][(n % PER) * G + i] = mma<T>(f[n & 1][i], b, acc[m][(n % PER) * G + i]);
+        }
         __builtin_amdgcn_sched_barrier(0);
     }
+}
+template <typename T, int DP>
+__device__ __forceinline__ void second_product(f32x4 (&acc)[DP / 16], const f32x4 (&w)[4], const Reader<T, DP>& rd,
+                                               const unsigned char* tile)
+{
+    second_products<T, DP, 1>(reinterpret_cast<f32x4 (&)[1][DP / 16]>(acc), reinterpret_cast<const f32x4 (&)[1][4]>(w), rd, tile);
 }
 
 // first[t] = streamed tile . owner, all 64 rows; the four blocks of rows side by side, since each is one chain of products.

@@ -28,11 +28,14 @@ template <typename T, int DP> struct DqShared {
 // One block: 64 queries of one head.  Dynamic LDS: kWavesPerBlock rows of 2 kNear + 1 sums of ds by distance.
 // KEEP > 0: histories of at most KEEP tiles; weights and products of the first walk stay in registers, and the second walk
 // loads the keys alone (queries of 1024 x 200, 8 heads of 128: 1.43 ms without).
-template <typename T, int DP, int UNIT, bool CAP, int WAVES, int KEEP>
+// TABLE: the table's gradient is wanted, and with it ds itself, so that delta_i = sum_j p_ij dp_ij comes first.  Otherwise one
+// walk does: bf16 rows take delta from dO . O, which knows O to 8 bits, sum p dp and p k on the way, and set dq right by
+// (dO . O - sum p dp) p k at the end; the products with p read no more of the tile.  float32 rows need none of that.
+template <typename T, int DP, int UNIT, bool CAP, int WAVES, bool TABLE, int KEEP>
 __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
 {
     using S = Shape<T, DP>;
-    constexpr bool AHEAD = S::RB < 256 && KEEP == 0;
+    constexpr bool AHEAD = S::RB < 256 && KEEP == 0, MEND = !TABLE && sizeof(T) == 2;
     extern __shared__ float dist[];
     __shared__ DqShared<T, DP> sh;
     const int item = xcd_item(a.items);
@@ -50,7 +53,6 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
     const T* const kp = static_cast<const T*>(a.k.data) + batch * a.k.sb + kvh * a.k.sh;
     const T* const vp = static_cast<const T*>(a.v.data) + batch * a.v.sb + kvh * a.v.sh;
     const int64_t stat = ((int64_t)batch * a.heads + head) * a.length + (q < a.length ? q : a.length - 1);
-    const bool want_table = a.part != nullptr;
 
     u32x4 qf[S::KK], df[S::KK];
     const int qseg = q < a.length ? row_segment(seg, q, a.length) : kNoSegOwner;
@@ -60,7 +62,7 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
     load_owner<T, DP, UNIT>(df, static_cast<const T*>(a.dout.data) + batch * a.dout.sb + head * a.dout.sh + wq0 * a.dout.sr,
                             a.dout.sr, a.length - wq0, a.dim, live, lane);
     float delta = 0.f;
-    if (!want_table) {
+    if constexpr (!TABLE) {
         u32x4 of[S::KK];
         load_owner<T, DP, UNIT>(of, static_cast<const T*>(a.o.data) + batch * a.o.sb + head * a.o.sh + wq0 * a.o.sr, a.o.sr,
                                 a.length - wq0, a.dim, live, lane);
@@ -105,17 +107,18 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
         feed.load(kp + k0 * a.k.sr, a.k.sr, vp + k0 * a.v.sr, a.v.sr, k0, a.length, seg, a.dim);
     };
     const int tfirst = next_tile(0, t1, mk);
-    const bool one_tile = want_table && next_tile(tfirst + 1, t1, mk) >= t1;
+    const bool one_tile = TABLE && next_tile(tfirst + 1, t1, mk) >= t1;
 
-    f32x4 dq[S::DT];
+    f32x4 dq[MEND ? 2 : 1][S::DT];                                // ds k, p k
 #pragma unroll
-    for (int dt = 0; dt < S::DT; ++dt) dq[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int dt = 0; dt < S::DT; ++dt) dq[0][dt] = dq[MEND ? 1 : 0][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float seen = 0.f;                                             // sum p dp
     // the distances that the block's pairs can have (table_near touches 76 below a pair of tiles), within kNear
     const int near_lo = q0 - (t1 - 1) * kTile - 76 > -kNear ? q0 - (t1 - 1) * kTile - 76 : -kNear;
     const int near_hi = q0 + kTile - 1 < kNear ? q0 + kTile - 1 : kNear;
     int flat_bucket = -1;
     float flat_sum = 0.f;
-    if (want_table) {
+    if constexpr (TABLE) {
         for (int n = near_lo + tid; n <= near_hi; n += kBlock)
 #pragma unroll
             for (int w = 0; w < kWavesPerBlock; ++w) dist[w * (2 * kNear + 1) + kNear + n] = 0.f;
@@ -124,7 +127,6 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
             for (int w = 0; w < kWavesPerBlock; ++w) sh.bucket[w][tid] = 0.f;
         delta = 0.f;
     }
-    // a tile's keys and values (or keys alone) to LDS
     auto flat_of = [&](int t) {
         const int hi = q0 + kTile - 1 - t * kTile;
         return a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
@@ -146,11 +148,11 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - lse2);
     };
-    auto add_delta = [&](const f32x4 (&s)[4], const f32x4 (&dp)[4]) {
+    auto add_seen = [&](const f32x4 (&s)[4], const f32x4 (&dp)[4]) {
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) delta += s[n][r] * dp[n][r];
+            for (int r = 0; r < 4; ++r) seen += s[n][r] * dp[n][r];
     };
     // ds in place of the weights, and what they add to the table's gradient
     auto table_sums = [&](int t, f32x4 (&s)[4], const f32x4 (&dp)[4]) {
@@ -158,7 +160,7 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
         for (int n = 0; n < 4; ++n)
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[n][r] *= dp[n][r] - delta;
-        if (!want_table) return;
+        if constexpr (!TABLE) return;
         const int flat = flat_of(t);
         if (flat >= 0) {
             if (flat != flat_bucket) {
@@ -190,22 +192,28 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
             if (AHEAD && tn < t1) load(tn);
             __syncthreads();
             if (sees(t)) {
-                f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
-                weigh(t, mixed, s, dp, slope);
-                if (DELTA || (want_table && one_tile)) add_delta(s, dp);
+                f32x4 s[MEND && !DELTA ? 2 : 1][4], dp[4], slope[CAP ? 4 : 1];
+                weigh(t, mixed, s[0], dp, slope);
+                if (DELTA || MEND || one_tile) add_seen(s[0], dp);
                 if constexpr (!DELTA) {
-                    if (want_table && one_tile) delta = group_sum(delta);
-                    table_sums(t, s, dp);
+                    if (one_tile) delta = group_sum(seen);
+                    if constexpr (MEND) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) s[1][n] = s[0][n];
+                    }
+                    table_sums(t, s[0], dp);
                     if constexpr (CAP) {
 #pragma unroll
-                        for (int n = 0; n < 4; ++n) s[n] *= slope[n];
+                        for (int m = 0; m <= (MEND ? 1 : 0); ++m)
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) s[m][n] *= slope[n];
                     }
-                    second_product<T, DP>(dq, s, rd, sh.k);
+                    second_products<T, DP>(dq, s, rd, sh.k);
                 }
             }
             t = tn;
         }
-        if constexpr (DELTA) delta = group_sum(delta);
+        if constexpr (DELTA) delta = group_sum(seen);
     };
     if constexpr (KEEP > 0) {
         f32x4 s[KEEP][4], dp[KEEP][4], none[1];
@@ -223,12 +231,12 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
                 __syncthreads();
                 if (sees(t)) {
                     weigh(t, mixed, s[i], dp[i], none);
-                    add_delta(s[i], dp[i]);
+                    add_seen(s[i], dp[i]);
                 }
                 t = next_tile(t + 1, t1, mk);
             }
         }
-        delta = group_sum(delta);
+        delta = group_sum(seen);
         bool there = true;                           // the keys of the last tile are in LDS still
 #pragma unroll
         for (int i = KEEP - 1; i >= 0; --i) {
@@ -243,20 +251,28 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
             there = false;
             if (sees(tile[i])) {
                 table_sums(tile[i], s[i], dp[i]);
-                second_product<T, DP>(dq, s[i], rd, sh.k);
+                second_product<T, DP>(dq[0], s[i], rd, sh.k);
             }
         }
     } else {
-        if (want_table && !one_tile) walk(std::true_type{});
+        if constexpr (TABLE) {
+            if (!one_tile) walk(std::true_type{});
+        }
         walk(std::false_type{});
+        if constexpr (MEND) {
+            seen = group_sum(seen);
+#pragma unroll
+            for (int dt = 0; dt < S::DT; ++dt) dq[0][dt] += (delta - seen) * dq[1][dt];
+            delta = seen;
+        }
     }
     __syncthreads();
     if (wq0 < a.length) {
         T* const dqp = static_cast<T*>(a.dq.data) + batch * a.dq.sb + head * a.dq.sh + wq0 * a.dq.sr;
-        store_rows<T, DP, UNIT>(sh.k + wave * 16 * S::RB, dq, a.scale, dqp, a.dq.sr, a.length - wq0, a.dim, lane);
+        store_rows<T, DP, UNIT>(sh.k + wave * 16 * S::RB, dq[0], a.scale, dqp, a.dq.sr, a.length - wq0, a.dim, lane);
         if (g == 0 && q < a.length) a.delta[stat] = delta;
     }
-    if (want_table) {
+    if constexpr (TABLE) {
         if (flat_bucket >= 0) add_bucket(sh.bucket[wave], flat_bucket, flat_sum, lane);
         __syncthreads();
         // bucket b of a side: the distances from its border to the next one's, eight lanes to a bucket; keys after the
@@ -292,19 +308,21 @@ void attend_backward_queries(const gram_attention_config& c, AttArgs a, int unit
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
         constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 3 : 2;
-        auto go = [&](auto keep) {
+        auto go = [&](auto table, auto keep) {
             constexpr int KEEP = decltype(keep)::value;
-            k_attend_dq<decltype(type), DP, decltype(u)::value, decltype(cap)::value, (KEEP > 2 ? 2 : WAVES), KEEP>
-                <<<att_grid(a.items), dim3(kBlock), dist, s>>>(a);
+            k_attend_dq<decltype(type), DP, decltype(u)::value, decltype(cap)::value, (KEEP > 2 ? 2 : WAVES), decltype(table)::value,
+                        KEEP><<<att_grid(a.items), dim3(kBlock), dist, s>>>(a);
         };
-        // kept are the tiles of histories of up to 256 positions, where there are two walks, no slopes to keep as well, and
-        // registers for it all: rows of 512 bytes leave none
+        const std::integral_constant<int, 0> none;
+        if (!a.part) return go(std::false_type{}, none);
+        // kept are the tiles of histories of up to 256 positions, where there are no slopes to keep as well and registers
+        // for it all: rows of 512 bytes leave none
         if constexpr (!decltype(cap)::value && Shape<decltype(type), DP>::RB <= 256) {
             const int tiles = att_blocks(a.length, kTile);
-            if (a.part && tiles == 2) return go(std::integral_constant<int, 2>{});
-            if (a.part && (tiles == 3 || tiles == 4)) return go(std::integral_constant<int, 4>{});
+            if (tiles == 2) return go(std::true_type{}, std::integral_constant<int, 2>{});
+            if (tiles == 3 || tiles == 4) return go(std::true_type{}, std::integral_constant<int, 4>{});
         }
-        go(std::integral_constant<int, 0>{});
+        go(std::true_type{}, none);
     });
 }
 
