@@ -35,7 +35,7 @@ template <typename T, int DP, int UNIT, bool CAP, int WAVES, bool TABLE, int KEE
 __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
 {
     using S = Shape<T, DP>;
-    constexpr bool AHEAD = S::RB < 256 && KEEP == 0, MEND = !TABLE && sizeof(T) == 2;
+    constexpr bool AHEAD = S::RB <= 256 && KEEP == 0, MEND = !TABLE && sizeof(T) == 2;
     extern __shared__ float dist[];
     __shared__ DqShared<T, DP> sh;
     const int item = xcd_item(a.items);
@@ -219,36 +219,43 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
         f32x4 s[KEEP][4], dp[KEEP][4], none[1];
         int tile[KEEP];
         int t = tfirst;
+        constexpr bool EARLY = KEEP > 2;             // the next tile's loads on their way: 1.03 ms and 1.09; two tiles would
+        if (EARLY) load(t < t1 ? t : 0);             // lose a wave per SIMD to it (1024 x 100, heads of 64: 15 us and 14)
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
             tile[i] = t;
             if (t < t1) {
                 const bool mixed = tile_mixed(mk, t);
-                load(t);
+                const int tn = next_tile(t + 1, t1, mk);
+                if (!EARLY) load(t);
                 __syncthreads();
                 feed.template put<false>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
                 put_bias(t);
+                if (EARLY && i + 1 < KEEP && tn < t1) load(tn);
                 __syncthreads();
                 if (sees(t)) {
                     weigh(t, mixed, s[i], dp[i], none);
                     add_seen(s[i], dp[i]);
                 }
-                t = next_tile(t + 1, t1, mk);
+                t = tn;
             }
         }
         delta = group_sum(seen);
+        auto load_keys = [&](int n) {
+            feed.template load<false>(kp + n * kTile * a.k.sr, a.k.sr, kp, a.k.sr, n * kTile, a.length, seg, a.dim);
+        };
         bool there = true;                           // the keys of the last tile are in LDS still
 #pragma unroll
         for (int i = KEEP - 1; i >= 0; --i) {
             if (tile[i] >= t1) continue;
             if (!there) {
-                const int k0 = tile[i] * kTile;
-                feed.template load<false>(kp + k0 * a.k.sr, a.k.sr, kp, a.k.sr, k0, a.length, seg, a.dim);
+                if (!EARLY) load_keys(tile[i]);
                 __syncthreads();
                 feed.template put<false, false>(sh.k, sh.v, sh.seg, !whole(tile[i], q0, tile_mixed(mk, tile[i])), nullptr);
                 __syncthreads();
             }
             there = false;
+            if (EARLY && i > 0) load_keys(tile[i - 1]);
             if (sees(tile[i])) {
                 table_sums(tile[i], s[i], dp[i]);
                 second_product<T, DP>(dq[0], s[i], rd, sh.k);
