@@ -29,20 +29,22 @@ __device__ __forceinline__ void spoil_rows(f32x4 (&s)[4], const uint32_t* bad, i
 
 // One block: 64 keys of one key head, 16 to a wave, against the queries of all heads of its group, one head after the
 // other.
-template <typename T, int DP, int UNIT, bool CAP, int WAVES>
-__global__ __launch_bounds__(kBlock, WAVES) void k_attend_dkv(const AttArgs a)
+template <typename T, int DP, int UNIT, bool CAP, int WAVES, int SPLIT>
+__global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttArgs a)
 {
     using S = Shape<T, DP>;
     constexpr bool AHEAD = S::RB < 256;
-    __shared__ DkvShared<T, DP> sh;
+    __shared__ DkvShared<T, DP> sets[SPLIT];
+    const int set = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kBlock) : 0;
+    DkvShared<T, DP>& sh = sets[set];
     const int item = xcd_item(a.items);
     if (item < 0) return;
-    const int tid = threadIdx.x, lane = lane_id();
+    const int tid = threadIdx.x % kBlock, lane = lane_id();
     const int ntiles = (a.length + kTile - 1) / kTile;
     const int rows_item = (int)a.by_tiles.quotient((uint32_t)item);       // history and key head
     const int kt = item - rows_item * ntiles;
     const int batch = (int)a.by_heads.quotient((uint32_t)rows_item), kvh = rows_item - batch * a.kv_heads;
-    const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int k0 = kt * kTile, wk0 = k0 + wave * 16, k = wk0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
     const int prefix = a.prefix ? a.prefix[batch] : 0;
@@ -86,35 +88,48 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dkv(const AttArgs a)
     for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (tid < 4) (&sh.bad[0][0])[tid] = 0u;
     int parity = 0;
-    int h = 0, t = next_tile(t0, ntiles, mk);
-    if (AHEAD && t < ntiles) load(0, t);
-    while (t < ntiles) {
-        if (!AHEAD) load(h, t);
-        const bool mixed = tile_mixed(mk, t);
+    struct Place {
+        int h, t;                                                 // t = ntiles: behind the last
+    };
+    const int tfirst = next_tile(t0, ntiles, mk);
+    auto after = [&](Place p) {
+        p.t = next_tile(p.t + 1, ntiles, mk);
+        if (p.t >= ntiles && p.h + 1 < a.group) p.h += 1, p.t = tfirst;
+        return p;
+    };
+    Place round = {0, tfirst}, at = set ? after(round) : round;   // the first set's tile and this one's
+    if (AHEAD && at.t < ntiles) load(at.h, at.t);
+    while (round.t < ntiles) {
+        const int h = at.h, t = at.t;
+        const bool there = SPLIT == 1 || t < ntiles;
+        if (!AHEAD && there) load(h, t);
+        const bool mixed = there && tile_mixed(mk, t);
         const int q0 = t * kTile, lo = q0 - (k0 + kTile - 1); // the smallest distance of the block's pairs
         const int flat = a.bk.side ? uniform_bucket(a.bk, lo, lo + 2 * kTile - 2) : 0;
         const float* const table = a.table + (int64_t)(kvh * a.group + h) * buckets;
         __syncthreads();
         const bool masked = !whole(t, k0 + kTile - 1, mixed);
-        feed.template put<false>(sh.q, sh.d, sh.seg, masked, sh.bad[parity]);
-        if (wave == 0) {
-            // a query whose statistics are not finite sees a non-finite value; it is marked like one that holds it
-            float lse2 = row_lse == -INFINITY || feed.seg == kNoSeg ? 0.f : row_lse * kLog2e, dl = feed.seg == kNoSeg ? 0.f : row_delta;
-            if (masked && (!(fabsf(lse2) < INFINITY) || !(fabsf(dl) < INFINITY))) {
-                lse2 = dl = 0.f;
-                atomicOr(&sh.bad[parity][lane >> 5], 1u << (lane & 31));
+        if (there) {
+            feed.template put<false>(sh.q, sh.d, sh.seg, masked, sh.bad[parity]);
+            if (wave == 0) {
+                // a query whose statistics are not finite sees a non-finite value; it is marked like one that holds it
+                float lse2 = row_lse == -INFINITY || feed.seg == kNoSeg ? 0.f : row_lse * kLog2e, dl = feed.seg == kNoSeg ? 0.f : row_delta;
+                if (masked && (!(fabsf(lse2) < INFINITY) || !(fabsf(dl) < INFINITY))) {
+                    lse2 = dl = 0.f;
+                    atomicOr(&sh.bad[parity][lane >> 5], 1u << (lane & 31));
+                }
+                sh.lse[lane] = lse2;
+                sh.delta[lane] = dl;
+                if (lane < 2) sh.bad[parity ^ 1][lane] = 0u;          // last read before the barrier above
             }
-            sh.lse[lane] = lse2;
-            sh.delta[lane] = dl;
-            if (lane < 2) sh.bad[parity ^ 1][lane] = 0u;          // last read before the barrier above
+            if (flat < 0 && tid < 2 * kTile - 1)
+                sh.bias[tid] = table[bucket_of(a.bk, sh.border, lo + tid)] * kLog2e;
         }
-        if (flat < 0 && tid < 2 * kTile - 1)
-            sh.bias[tid] = table[bucket_of(a.bk, sh.border, lo + tid)] * kLog2e;
-        int hn = h, tn = next_tile(t + 1, ntiles, mk);
-        if (tn >= ntiles && h + 1 < a.group) hn = h + 1, tn = next_tile(t0, ntiles, mk);
-        if (AHEAD && tn < ntiles) load(hn, tn);
+        round = after(SPLIT > 1 ? after(round) : round);
+        at = set ? after(round) : round;
+        if (AHEAD && at.t < ntiles) load(at.h, at.t);
         __syncthreads();
-        const bool sees = wk0 < a.length && !(a.causal && q0 + kTile - 1 < wk0 && wk0 >= prefix);
+        const bool sees = there && wk0 < a.length && !(a.causal && q0 + kTile - 1 < wk0 && wk0 >= prefix);
         if (sees) {
             f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
             first_product<T, DP>(s, kf, rd, sh.q);
@@ -143,9 +158,21 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dkv(const AttArgs a)
             second_product<T, DP>(dk, dp, rd, sh.q);
         }
         parity ^= 1;
-        h = hn, t = tn;
     }
     __syncthreads();
+    if constexpr (SPLIT > 1) {
+        if (set) {
+            hand_over(sets[1].q, dk, wave, lane);                 // and the rows of do behind
+            hand_over(sets[0].q, dv, wave, lane);
+        }
+        __syncthreads();
+        if (!set) {
+            take_over(sets[1].q, dk, 1.f, 1.f, wave, lane);
+            take_over(sets[0].q, dv, 1.f, 1.f, wave, lane);
+        }
+        __syncthreads();
+        if (set) return;
+    }
     if (wk0 < a.length) {
         T* const dkp = static_cast<T*>(a.dk.data) + batch * a.dk.sb + kvh * a.dk.sh + wk0 * a.dk.sr;
         T* const dvp = static_cast<T*>(a.dv.data) + batch * a.dv.sb + kvh * a.dv.sh + wk0 * a.dv.sr;
@@ -164,7 +191,14 @@ void attend_backward_keys(const gram_attention_config& c, AttArgs a, int unit, h
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
         constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 3 : 2;
-        k_attend_dkv<decltype(type), DP, decltype(u)::value, decltype(cap)::value, WAVES><<<att_grid(a.items), dim3(kBlock), 0, s>>>(a);
+        auto go = [&](auto split) {
+            constexpr int SPLIT = decltype(split)::value;
+            k_attend_dkv<decltype(type), DP, decltype(u)::value, decltype(cap)::value, (SPLIT > 1 ? 2 : WAVES), SPLIT>
+                <<<att_grid(a.items), dim3(kBlock * SPLIT), 0, s>>>(a);
+        };
+        if constexpr (Shape<decltype(type), DP>::RB <= 256)
+            if (a.items <= kFewBlocks && a.length > kTile) return go(std::integral_constant<int, 2>{});
+        go(std::integral_constant<int, 1>{});
     });
 }
 

@@ -31,22 +31,24 @@ template <typename T, int DP> struct DqShared {
 // TABLE: the table's gradient is wanted, and with it ds itself, so that delta_i = sum_j p_ij dp_ij comes first.  Otherwise one
 // walk does: bf16 rows take delta from dO . O, which knows O to 8 bits, sum p dp and p k on the way, and set dq right by
 // (dO . O - sum p dp) p k at the end; the products with p read no more of the tile.  float32 rows need none of that.
-template <typename T, int DP, int UNIT, bool CAP, int WAVES, bool TABLE, int KEEP>
-__global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
+template <typename T, int DP, int UNIT, bool CAP, int WAVES, bool TABLE, int KEEP, int SPLIT>
+__global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttArgs a)
 {
     using S = Shape<T, DP>;
     constexpr bool AHEAD = S::RB <= 256 && KEEP == 0, MEND = !TABLE && sizeof(T) == 2;
     extern __shared__ float dist[];
-    __shared__ DqShared<T, DP> sh;
+    __shared__ DqShared<T, DP> sets[SPLIT];
+    const int set = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kBlock) : 0;
+    DqShared<T, DP>& sh = sets[set];
     const int item = xcd_item(a.items);
     if (item < 0) return;
-    const int tid = threadIdx.x, lane = lane_id();
+    const int tid = threadIdx.x % kBlock, lane = lane_id();
     const int nqt = (a.length + kTile - 1) / kTile;
     const int rows_item = (int)a.by_tiles.quotient((uint32_t)item);       // history and head
     const int qt = nqt - 1 - (item - rows_item * nqt);
     const int batch = (int)a.by_heads.quotient((uint32_t)rows_item), head = rows_item - batch * a.heads;
     const int kvh = (int)a.by_group.quotient((uint32_t)head);
-    const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int q0 = qt * kTile, wq0 = q0 + wave * 16, q = wq0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
     const int prefix = a.prefix ? a.prefix[batch] : 0;
@@ -86,7 +88,8 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
     if (tid < kMaxBorders) sh.border[tid] = kernel_borders()[tid];
     if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;
-    float* const my_dist = dist + wave * (2 * kNear + 1) + kNear;
+    constexpr int kRows = kWavesPerBlock * SPLIT;                 // of sums by distance
+    float* const my_dist = dist + (set * kWavesPerBlock + wave) * (2 * kNear + 1) + kNear;
 
     const Reader<T, DP> rd(lane);
     Feed<T, DP, UNIT> feed(tid);
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
     if constexpr (TABLE) {
         for (int n = near_lo + tid; n <= near_hi; n += kBlock)
 #pragma unroll
-            for (int w = 0; w < kWavesPerBlock; ++w) dist[w * (2 * kNear + 1) + kNear + n] = 0.f;
+            for (int w = set * kWavesPerBlock; w < (set + 1) * kWavesPerBlock; ++w) dist[w * (2 * kNear + 1) + kNear + n] = 0.f;
         for (int i = tid; i < kWavesPerBlock * 4 * kStrip; i += kBlock) (&sh.strip[0][0][0])[i] = 0.f;
         if (tid < kMaxBorders)
             for (int w = 0; w < kWavesPerBlock; ++w) sh.bucket[w][tid] = 0.f;
@@ -180,18 +183,22 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
     // DELTA: only sum p dp; else the gradients, with that sum on the way where the one tile holds it all
     auto walk = [&](auto delta_only) {
         constexpr bool DELTA = decltype(delta_only)::value;
-        int t = tfirst;
+        auto after = [&](int t) { return next_tile(t + 1, t1, mk); };
+        int round = tfirst, t = set ? after(round) : round;       // the first set's tile and this one's
         if (AHEAD && t < t1) load(t);
-        while (t < t1) {
-            const bool mixed = tile_mixed(mk, t);
-            if (!AHEAD) load(t);
+        while (round < t1) {
+            const bool there = SPLIT == 1 || t < t1, mixed = there && tile_mixed(mk, t);
+            if (!AHEAD && there) load(t);
             __syncthreads();
-            feed.template put<false>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
-            put_bias(t);
-            const int tn = next_tile(t + 1, t1, mk);
+            if (there) {
+                feed.template put<false>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
+                put_bias(t);
+            }
+            round = after(SPLIT > 1 ? after(round) : round);
+            const int tn = set ? after(round) : round;
             if (AHEAD && tn < t1) load(tn);
             __syncthreads();
-            if (sees(t)) {
+            if (there && sees(t)) {
                 f32x4 s[MEND && !DELTA ? 2 : 1][4], dp[4], slope[CAP ? 4 : 1];
                 weigh(t, mixed, s[0], dp, slope);
                 if (DELTA || MEND || one_tile) add_seen(s[0], dp);
@@ -213,7 +220,15 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
             }
             t = tn;
         }
-        if constexpr (DELTA) delta = group_sum(seen);
+        if constexpr (DELTA) {
+            delta = group_sum(seen);
+            if constexpr (SPLIT > 1) {
+                __syncthreads();                                  // the bias has been read
+                sh.bias[wave * 16 + c] = delta;
+                __syncthreads();
+                delta = sets[0].bias[wave * 16 + c] + sets[1].bias[wave * 16 + c];
+            }
+        }
     };
     if constexpr (KEEP > 0) {
         f32x4 s[KEEP][4], dp[KEEP][4], none[1];
@@ -266,15 +281,31 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
             if (!one_tile) walk(std::true_type{});
         }
         walk(std::false_type{});
+        if constexpr (SPLIT > 1) {
+            __syncthreads();
+            if (set) {
+                hand_over(sets[1].k, dq[0], wave, lane);          // and the values behind
+                if constexpr (MEND) {
+                    hand_over(sets[0].k, dq[1], wave, lane);
+                    seen = group_sum(seen);
+                    sets[1].bias[wave * 16 + c] = seen;
+                }
+            }
+            __syncthreads();
+            if (!set) {
+                take_over(sets[1].k, dq[0], 1.f, 1.f, wave, lane);
+                if constexpr (MEND) take_over(sets[0].k, dq[1], 1.f, 1.f, wave, lane);
+            }
+        }
         if constexpr (MEND) {
-            seen = group_sum(seen);
+            seen = group_sum(seen) + (SPLIT > 1 ? sets[SPLIT - 1].bias[wave * 16 + c] : 0.f);
 #pragma unroll
             for (int dt = 0; dt < S::DT; ++dt) dq[0][dt] += (delta - seen) * dq[1][dt];
             delta = seen;
         }
     }
     __syncthreads();
-    if (wq0 < a.length) {
+    if (set == 0 && wq0 < a.length) {
         T* const dqp = static_cast<T*>(a.dq.data) + batch * a.dq.sb + head * a.dq.sh + wq0 * a.dq.sr;
         store_rows<T, DP, UNIT>(sh.k + wave * 16 * S::RB, dq[0], a.scale, dqp, a.dq.sr, a.length - wq0, a.dim, lane);
         if (g == 0 && q < a.length) a.delta[stat] = delta;
@@ -286,8 +317,13 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
         // query count as distance 0 where there is one side
         const float* const row = dist + kNear;
         constexpr int W = 2 * kNear + 1;
-        auto at = [&](int n) { return (row[n] + row[W + n]) + (row[2 * W + n] + row[3 * W + n]); };
-        for (int b = tid >> 3; b < buckets; b += kBlock / 8) {
+        auto at = [&](int n) {
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kRows; w += 4) sum += (row[w * W + n] + row[(w + 1) * W + n]) + (row[(w + 2) * W + n] + row[(w + 3) * W + n]);
+            return sum;
+        };
+        for (int b = threadIdx.x >> 3; b < buckets; b += kBlock * SPLIT / 8) {
             const int sub = tid & 7;
             const bool after = b >= a.bk.side;
             const int i = (after ? b - a.bk.side : b) - a.bk.exact, most = after ? -near_lo : near_hi;
@@ -295,7 +331,7 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend_dq(const AttArgs a)
             int to = i < 0 ? from + 1 : i < a.bk.borders ? sh.border[i] : kNear + 1;
             to = to < most + 1 ? to : most + 1;
             if (after && from == 0) from = 1;
-            float sum = sub < kWavesPerBlock ? sh.bucket[sub][b] : 0.f;
+            float sum = sub < kRows ? sets[sub / kWavesPerBlock].bucket[sub % kWavesPerBlock][b] : 0.f;
             for (int n = from + sub; n < to; n += 8) sum += at(after ? -n : n);
             if (b == 0 && !a.bk.two_sided)
                 for (int n = 1 + sub; n <= -near_lo; n += 8) sum += at(-n);
@@ -311,25 +347,31 @@ void attend_backward_queries(const gram_attention_config& c, AttArgs a, int unit
 {
     a.items = a.batch * a.heads * att_blocks(a.length, kTile);
     a.by_tiles = FastDiv::of(att_blocks(a.length, kTile)), a.by_heads = FastDiv::of(a.heads), a.by_group = FastDiv::of(a.group);
-    const size_t dist = a.part ? kWavesPerBlock * (2 * kNear + 1) * sizeof(float) : 0;
+    const bool few = a.items <= kFewBlocks && a.length > kTile;
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
         constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 3 : 2;
-        auto go = [&](auto table, auto keep) {
-            constexpr int KEEP = decltype(keep)::value;
-            k_attend_dq<decltype(type), DP, decltype(u)::value, decltype(cap)::value, (KEEP > 2 ? 2 : WAVES), decltype(table)::value,
-                        KEEP><<<att_grid(a.items), dim3(kBlock), dist, s>>>(a);
+        auto go = [&](auto table, auto keep, auto split) {
+            constexpr int KEEP = decltype(keep)::value, SPLIT = decltype(split)::value;
+            const size_t dist = a.part ? SPLIT * kWavesPerBlock * (2 * kNear + 1) * sizeof(float) : 0;
+            k_attend_dq<decltype(type), DP, decltype(u)::value, decltype(cap)::value, (KEEP > 2 || SPLIT > 1 ? 2 : WAVES),
+                        decltype(table)::value, KEEP, SPLIT><<<att_grid(a.items), dim3(kBlock * SPLIT), dist, s>>>(a);
         };
         const std::integral_constant<int, 0> none;
-        if (!a.part) return go(std::false_type{}, none);
+        const std::integral_constant<int, 1> one;
+        if constexpr (Shape<decltype(type), DP>::RB <= 256) {
+            const std::integral_constant<int, 2> two;
+            if (few) return a.part ? go(std::true_type{}, none, two) : go(std::false_type{}, none, two);
+        }
+        if (!a.part) return go(std::false_type{}, none, one);
         // kept are the tiles of histories of up to 256 positions, where there are no slopes to keep as well and registers
         // for it all: rows of 512 bytes leave none
         if constexpr (!decltype(cap)::value && Shape<decltype(type), DP>::RB <= 256) {
             const int tiles = att_blocks(a.length, kTile);
-            if (tiles == 2) return go(std::true_type{}, std::integral_constant<int, 2>{});
-            if (tiles == 3 || tiles == 4) return go(std::true_type{}, std::integral_constant<int, 4>{});
+            if (tiles == 2) return go(std::true_type{}, std::integral_constant<int, 2>{}, one);
+            if (tiles == 3 || tiles == 4) return go(std::true_type{}, std::integral_constant<int, 4>{}, one);
         }
-        go(std::true_type{}, none);
+        go(std::true_type{}, none, one);
     });
 }
 

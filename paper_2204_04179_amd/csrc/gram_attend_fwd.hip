@@ -21,21 +21,23 @@ template <typename T, int DP> struct FwdShared {
 };
 
 // One block: 64 queries of one head, 16 to a wave.
-template <typename T, int DP, int UNIT, bool CAP, int WAVES>
-__global__ __launch_bounds__(kBlock, WAVES) void k_attend(const AttArgs a)
+template <typename T, int DP, int UNIT, bool CAP, int WAVES, int SPLIT>
+__global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend(const AttArgs a)
 {
     using S = Shape<T, DP>;
     constexpr bool AHEAD = S::RB < 256;          // the next tile's loads under way while this one is worked on
-    __shared__ FwdShared<T, DP> sh;
+    __shared__ FwdShared<T, DP> sets[SPLIT];
+    const int set = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kBlock) : 0;
+    FwdShared<T, DP>& sh = sets[set];
     const int item = xcd_item(a.items);
     if (item < 0) return;
-    const int tid = threadIdx.x, lane = lane_id();
+    const int tid = threadIdx.x % kBlock, lane = lane_id();
     const int nqt = (a.length + kTile - 1) / kTile;
     const int rows_item = (int)a.by_tiles.quotient((uint32_t)item);       // history and head
     const int qt = nqt - 1 - (item - rows_item * nqt);                 // the longest rows of a causal mask first
     const int batch = (int)a.by_heads.quotient((uint32_t)rows_item), head = rows_item - batch * a.heads;
     const int kvh = (int)a.by_group.quotient((uint32_t)head);
-    const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int q0 = qt * kTile, wq0 = q0 + wave * 16, q = wq0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
     const int prefix = a.prefix ? a.prefix[batch] : 0;
@@ -83,21 +85,25 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend(const AttArgs a)
     float top = -INFINITY, total = 0.f;
 #pragma unroll
     for (int dt = 0; dt < S::DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    int t = next_tile(0, t1, mk);
+    auto after = [&](int t) { return next_tile(t + 1, t1, mk); };
+    int round = next_tile(0, t1, mk), t = set ? after(round) : round;     // the first set's tile and this one's
     if (AHEAD && t < t1) load(t);
-    while (t < t1) {
-        const bool mixed = tile_mixed(mk, t);
+    while (round < t1) {
+        const bool there = SPLIT == 1 || t < t1, mixed = there && tile_mixed(mk, t);
         const int k0 = t * kTile, hi = q0 + kTile - 1 - k0;   // the largest distance of the block's pairs
         const int flat = a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
-        if (!AHEAD) load(t);
+        if (!AHEAD && there) load(t);
         __syncthreads();                                      // the tile before has been read
-        feed.template put<true>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
-        if (flat < 0 && tid < 2 * kTile - 1)
-            sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, hi - tid)];
-        const int tn = next_tile(t + 1, t1, mk);
+        if (there) {
+            feed.template put<true>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
+            if (flat < 0 && tid < 2 * kTile - 1)
+                sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, hi - tid)];
+        }
+        round = after(SPLIT > 1 ? after(round) : round);
+        const int tn = set ? after(round) : round;
         if (AHEAD && tn < t1) load(tn);
         __syncthreads();
-        if (wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix)) {
+        if (there && wq0 < a.length && !(a.causal && k0 > wq0 + 15 && k0 >= prefix)) {
             f32x4 s[4], slope[CAP ? 4 : 1];
             first_product<T, DP>(s, qf, rd, sh.k);
             to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? sh.table[flat] : 0.f);
@@ -132,6 +138,22 @@ __global__ __launch_bounds__(kBlock, WAVES) void k_attend(const AttArgs a)
     }
     total = group_sum(total);
     __syncthreads();                                              // the tiles have been read
+    if constexpr (SPLIT > 1) {
+        unsigned char* const room = sets[1].k;                    // and the values behind
+        float* const stats = &sets[1].bias[2 * (wave * 16 + c)];
+        if (set) {
+            hand_over(room, o, wave, lane);
+            stats[0] = top, stats[1] = total;
+        }
+        __syncthreads();
+        if (set) return;
+        const float other = stats[0], most = fmaxf(top, other);
+        const float mine = top == most ? 1.f : __builtin_amdgcn_exp2f(top - most);
+        const float theirs = other == most ? 1.f : __builtin_amdgcn_exp2f(other - most);
+        take_over(room, o, mine, theirs, wave, lane);
+        total = total * mine + stats[1] * theirs;
+        top = most;
+    }
     if (wq0 < a.length) {
         const bool empty = top == -INFINITY && total == 0.f;
         T* const op = static_cast<T*>(a.o.data) + batch * a.o.sb + head * a.o.sh + wq0 * a.o.sr;
@@ -151,7 +173,14 @@ void attend_forward(const gram_attention_config& c, AttArgs a, int unit, hipStre
         constexpr int DP = decltype(dp)::value;
         // blocks per CU that registers allow: accumulators, fragments and the tile under way grow with the row's bytes
         constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 4 : Shape<decltype(type), DP>::RB <= 256 ? 3 : 2;
-        k_attend<decltype(type), DP, decltype(u)::value, decltype(cap)::value, WAVES><<<att_grid(a.items), dim3(kBlock), 0, s>>>(a);
+        auto go = [&](auto split) {
+            constexpr int SPLIT = decltype(split)::value;
+            k_attend<decltype(type), DP, decltype(u)::value, decltype(cap)::value, (SPLIT > 1 ? 2 : WAVES), SPLIT>
+                <<<att_grid(a.items), dim3(kBlock * SPLIT), 0, s>>>(a);
+        };
+        if constexpr (Shape<decltype(type), DP>::RB <= 256)
+            if (a.items <= kFewBlocks && a.length > kTile) return go(std::integral_constant<int, 2>{});
+        go(std::integral_constant<int, 1>{});
     });
 }
 

@@ -161,6 +161,28 @@ def test_attention_and_its_backward(c):
         lo.assert_within(got[n], want[n], n)
 
 
+# More blocks of 64 rows than the GPU has CUs, where a block is four waves rather than eight, over two, three, four and
+# more tiles of a history.
+MANY = [
+    case("bf16", 40, 100, 4, 4, 64, pad="tail", buckets=32, far=128), case("f32", 65, 70, 2, 2, 24, prefix=True, docs=True, buckets=12, far=40, both=True),
+    case("bf16", 50, 200, 2, 2, 128, docs=True, pad="holes", buckets=32, far=128),
+    case("f32", 35, 150, 4, 4, 64, causal=False, buckets=16, far=40, both=True),
+    case("bf16", 33, 260, 4, 2, 36, docs=True, cap=5.0, buckets=32, far=100), case("bf16", 52, 300, 1, 1, 128, docs=True),
+    case("bf16", 33, 260, 2, 2, 20, causal=False, pad="tail", buckets=64, far=100), case("f32", 44, 129, 2, 2, 40, cap=30.0),
+    case("f32", 20, 257, 6, 3, 100, pad="all", buckets=32, far=128), case("bf16", 130, 120, 2, 1, 64, pad="holes", layout="heads"),
+]
+
+
+@pytest.mark.parametrize("c", MANY, ids=name_of)
+def test_attention_and_its_backward_of_many_histories(c):
+    test_attention_and_its_backward(c)
+
+
+@pytest.mark.parametrize("c", MANY[:6], ids=name_of)
+def test_non_finite_values_among_many_histories(c):
+    test_non_finite_values_reach_only_those_that_see_them(c, "all")
+
+
 # ---- one cached step --------------------------------------------------------------------------------------
 
 STEPS = [
