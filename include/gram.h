@@ -435,6 +435,7 @@ int gram_layer_norm_backward(const void* x, int32_t x_dtype, const float* weight
  * buckets / 2, keys after the query have bucket S + bucket(j - i).
  * gram_distance_bucket (HOST only) returns the bucket of i - j = distance, or -1. */
 #define GRAM_ATTENTION_MAX_LENGTH 262144
+#define GRAM_ATTENTION_MAX_CAPACITY (1 << 30)
 #define GRAM_ATTENTION_MAX_BUCKETS 64
 typedef struct gram_attention_config {
     int32_t heads;         /* query heads, a multiple of kv_heads (1..65535)          */
@@ -451,9 +452,12 @@ typedef struct gram_attention_config {
 
 /* Rows of an operand: element e of head h at row p of history b is
  * data[b * batch_stride + p * row_stride + h * head_stride + e] (strides in
- * elements).  Packed projections and caches are passed as they lie.  Where all
- * operands of a call have 16-byte aligned rows, loads move 16 bytes (bf16 rows
- * aligned to 8 bytes: 8), else single elements. */
+ * elements; the stride of something that there is one of is not looked at).
+ * Packed projections and caches are passed as they lie.  Strides are >= 0 and
+ * rows less than 64 MiB apart; the rows of an operand that is written do not
+ * overlap one another or any other operand.  Where all operands of a call have
+ * 16-byte aligned rows, loads move 16 bytes (bf16 rows aligned to 8 bytes: 8),
+ * else single elements. */
 typedef struct gram_rows {
     void* data;
     int64_t batch_stride, row_stride, head_stride;
@@ -495,9 +499,11 @@ int gram_attention_backward(const gram_attention_config* cfg, int32_t batch, int
 /* Serving: one new item per history.  The new key and value are written to row
  * lengths[b] of history b's cache and the new query, at that position, attends to
  * rows first[b] .. lengths[b].
- *   q, o     [batch, 1, heads, head_dim] (row_stride unused)
+ *   q, o     [batch, 1, heads, head_dim] (row_stride unused; heads of q less than
+ *            64 MiB apart)
  *   k_new, v_new      [batch, 1, kv_heads, head_dim] (row_stride unused)
- *   k_cache, v_cache  [batch, capacity, kv_heads, head_dim]
+ *   k_cache, v_cache  [batch, capacity, kv_heads, head_dim], capacity at most
+ *            GRAM_ATTENTION_MAX_CAPACITY
  *   lengths  DEVICE [batch]  items that the cache holds; outside [0, capacity) the
  *            history is idle: its o is zero and its cache is left as it is.  The
  *            caller advances lengths after the last layer

@@ -468,6 +468,13 @@ __device__ __forceinline__ int row_segment(const int* __restrict__ seg, int row,
     return v < 0 ? kNoSeg : v;
 }
 
+// A history's prefix, clipped to its length: sums with it stay in range whatever the entry holds.
+__device__ __forceinline__ int prefix_of(const int* __restrict__ prefix, int batch, int length)
+{
+    const int p = prefix ? prefix[batch] : 0;
+    return p < length ? p : length;
+}
+
 struct TileMarks {
     uint32_t active[kAttMaxTiles / 32], mixed[kAttMaxTiles / 32];
     int red[12];

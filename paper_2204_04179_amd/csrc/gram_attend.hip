@@ -85,35 +85,47 @@ const char* check_sizes(const gram_attention_config* c, int32_t batch, int32_t l
 
 // Bytes per global access that addresses and strides of every operand allow: 16, 8 (bf16), or one element.
 struct UnitFinder {
+    int es, dim;
+    int64_t batch;
     uint64_t bits = 0;
-    bool null = false, far = false;
-    AttRows add(const gram_rows* r, int es)
+    bool null = false, far = false, shared = false;
+    UnitFinder(const gram_attention_config& c, int32_t batch) : es(c.dtype == GRAM_BF16 ? 2 : 4), dim(c.head_dim), batch(batch) {}
+    AttRows add(const gram_rows* r, int64_t rows, int64_t heads, bool written = false)
     {
         AttRows out{};
         if (!r || !r->data) {
             null = true;
             return out;
         }
-        out.data = r->data, out.sb = r->batch_stride, out.sr = r->row_stride, out.sh = r->head_stride;
-        far |= out.sr < 0 || out.sr * es >= kAttMaxRowBytes || out.sb < 0 || out.sh < 0;
-        bits |= reinterpret_cast<uintptr_t>(r->data) | (uint64_t)(out.sb * es) | (uint64_t)(out.sr * es) | (uint64_t)(out.sh * es);
+        out.data = r->data;
+        out.sb = stride(r->batch_stride, batch, INT64_MAX, written);
+        out.sr = stride(r->row_stride, rows, kAttMaxRowBytes / es, written);
+        out.sh = stride(r->head_stride, heads, INT64_MAX, written);
+        bits |= reinterpret_cast<uintptr_t>(r->data) | (uint64_t)((out.sb | out.sr | out.sh) * es);
         return out;
     }
-    int unit(int dim, int es) const
+    // a stride of something that there is one of has no meaning
+    int64_t stride(int64_t s, int64_t count, int64_t end, bool written)
+    {
+        if (count <= 1) return 0;
+        far |= s < 0 || s >= end;
+        shared |= written && s < dim;
+        return s;
+    }
+    int unit() const
     {
         const uint64_t all = bits | (uint64_t)(dim * es);
         return (all & 15) == 0 ? 16 : es == 2 && (all & 7) == 0 ? 8 : es;
     }
-    const char* refusal(int es) const
+    const char* refusal() const
     {
         if (null) return "NULL pointer";
         if (bits & (uint64_t)(es - 1)) return "an operand is not aligned to its elements";
         if (far) return "strides must be >= 0 and rows less than 64 MiB apart";
+        if (shared) return "rows of an operand that is written must not overlap";
         return nullptr;
     }
 };
-
-int elem_size(const gram_attention_config& c) { return c.dtype == GRAM_BF16 ? 2 : 4; }
 
 void fill(AttArgs& a, const gram_attention_config& c, int32_t batch, int32_t length)
 {
@@ -152,15 +164,15 @@ int gram_attention(const gram_attention_config* cfg, int32_t batch, int32_t leng
     if (const char* why = check_sizes(cfg, batch, length)) return fail_call(GRAM_ERR_ARG, "gram_attention: %s", why);
     if (prefix && !cfg->causal) return fail_call(GRAM_ERR_ARG, "gram_attention: a prefix needs the causal mask");
     if (batch == 0 || length == 0) return GRAM_OK;
-    const int es = elem_size(*cfg);
     AttArgs a{};
-    UnitFinder u;
-    a.q = u.add(q, es), a.k = u.add(k, es), a.v = u.add(v, es), a.o = u.add(o, es);
-    if (const char* why = cfg->buckets > 0 && !table ? "NULL pointer" : u.refusal(es))
+    UnitFinder u(*cfg, batch);
+    const int64_t H = cfg->heads, KV = cfg->kv_heads;
+    a.q = u.add(q, length, H), a.k = u.add(k, length, KV), a.v = u.add(v, length, KV), a.o = u.add(o, length, H, true);
+    if (const char* why = cfg->buckets > 0 && !table ? "NULL pointer" : u.refusal())
         return fail_call(GRAM_ERR_ARG, "gram_attention: %s", why);
     fill(a, *cfg, batch, length);
     a.seg = segments, a.prefix = prefix, a.table = table, a.lse = lse;
-    attend_forward(*cfg, a, u.unit(a.dim, es), static_cast<hipStream_t>(stream));
+    attend_forward(*cfg, a, u.unit(), static_cast<hipStream_t>(stream));
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? GRAM_OK : fail_call(GRAM_ERR_HIP, "gram_attention: %s", hipGetErrorString(e));
 }
@@ -186,13 +198,14 @@ int gram_attention_backward(const gram_attention_config* cfg, int32_t batch, int
         return fail_call(GRAM_ERR_ARG, "gram_attention_backward: dtable without buckets");
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool none = batch == 0 || length == 0;
-    const int es = elem_size(*cfg);
     AttArgs a{};
     if (!none) {
-        UnitFinder u;
-        a.q = u.add(q, es), a.k = u.add(k, es), a.v = u.add(v, es), a.o = u.add(o, es), a.dout = u.add(dout, es);
-        a.dq = u.add(dq, es), a.dk = u.add(dk, es), a.dv = u.add(dv, es);
-        if (const char* why = !lse || !work || (cfg->buckets > 0 && !table) ? "NULL pointer" : u.refusal(es))
+        UnitFinder u(*cfg, batch);
+        const int64_t H = cfg->heads, KV = cfg->kv_heads;
+        a.q = u.add(q, length, H), a.k = u.add(k, length, KV), a.v = u.add(v, length, KV), a.o = u.add(o, length, H);
+        a.dout = u.add(dout, length, H);
+        a.dq = u.add(dq, length, H, true), a.dk = u.add(dk, length, KV, true), a.dv = u.add(dv, length, KV, true);
+        if (const char* why = !lse || !work || (cfg->buckets > 0 && !table) ? "NULL pointer" : u.refusal())
             return fail_call(GRAM_ERR_ARG, "gram_attention_backward: %s", why);
         if ((reinterpret_cast<uintptr_t>(work) & 15) != 0)
             return fail_call(GRAM_ERR_ARG, "gram_attention_backward: work must be 16-byte aligned");
@@ -203,7 +216,7 @@ int gram_attention_backward(const gram_attention_config* cfg, int32_t batch, int
                                                    up256((int64_t)batch * cfg->heads * length * (int64_t)sizeof(float)))
                         : nullptr;
         a.parts = batch * att_blocks(length, kTile);
-        const int unit = u.unit(cfg->head_dim, es);
+        const int unit = u.unit();
         if (!attend_backward_short(*cfg, a, unit, s)) {
             attend_backward_queries(*cfg, a, unit, s);  // also leaves delta for the pass over the keys
             attend_backward_keys(*cfg, a, unit, s);
@@ -218,7 +231,7 @@ int gram_attention_backward(const gram_attention_config* cfg, int32_t batch, int
 
 int64_t gram_attention_step_bytes(const gram_attention_config* cfg, int32_t batch, int32_t capacity)
 {
-    if (check_config(cfg) || batch < 0 || capacity < 1) return 0;
+    if (check_config(cfg) || batch < 0 || capacity < 1 || capacity > GRAM_ATTENTION_MAX_CAPACITY) return 0;
     return (batch ? step_part_bytes(*cfg, batch, capacity) : 0) + 256;
 }
 
@@ -228,22 +241,23 @@ int gram_attention_step(const gram_attention_config* cfg, int32_t batch, int32_t
                         void* stream)
 {
     if (const char* why = check_config(cfg)) return fail_call(GRAM_ERR_ARG, "gram_attention_step: %s", why);
-    if (batch < 0 || capacity < 1) return fail_call(GRAM_ERR_ARG, "gram_attention_step: batch must be >= 0 and capacity >= 1");
+    if (batch < 0 || capacity < 1 || capacity > GRAM_ATTENTION_MAX_CAPACITY)
+        return fail_call(GRAM_ERR_ARG, "gram_attention_step: batch must be >= 0 and capacity in [1, 2^30]");
     if (batch == 0) return GRAM_OK;
-    const int es = elem_size(*cfg);
-    UnitFinder u;
-    const AttRows rq = u.add(q, es), rkn = u.add(k_new, es), rvn = u.add(v_new, es), rkc = u.add(k_cache, es),
-                  rvc = u.add(v_cache, es), ro = u.add(o, es);
+    UnitFinder u(*cfg, batch);
+    const int64_t H = cfg->heads, KV = cfg->kv_heads;
+    const AttRows rq = u.add(q, 1, H), rkn = u.add(k_new, 1, KV), rvn = u.add(v_new, 1, KV),
+                  rkc = u.add(k_cache, capacity, KV, true), rvc = u.add(v_cache, capacity, KV, true), ro = u.add(o, 1, H, true);
     const bool null = !lengths || (cfg->buckets > 0 && !table) || (!work && step_part_bytes(*cfg, batch, capacity) > 0);
-    if (const char* why = null ? "NULL pointer" : u.refusal(es)) return fail_call(GRAM_ERR_ARG, "gram_attention_step: %s", why);
-    if (rq.sh * es >= kAttMaxRowBytes)      // the heads of a query are the rows of an operand
+    if (const char* why = null ? "NULL pointer" : u.refusal()) return fail_call(GRAM_ERR_ARG, "gram_attention_step: %s", why);
+    if (rq.sh >= kAttMaxRowBytes / u.es)    // the heads of a query are the rows of an operand
         return fail_call(GRAM_ERR_ARG, "gram_attention_step: the heads of q must be less than 64 MiB apart");
     if ((reinterpret_cast<uintptr_t>(work) & 15) != 0)
         return fail_call(GRAM_ERR_ARG, "gram_attention_step: work must be 16-byte aligned");
     AttBuckets bk;
     make_buckets(*cfg, &bk);
     if (!step_launch(*cfg, bk, batch, capacity, rq, rkn, rvn, rkc, rvc, ro, lengths, first, table, work,
-                     u.unit(cfg->head_dim, es), static_cast<hipStream_t>(stream)))
+                     u.unit(), static_cast<hipStream_t>(stream)))
         return fail_call(GRAM_ERR_ARG, "gram_attention_step: batch * heads must be at most 2^23");
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? GRAM_OK : fail_call(GRAM_ERR_HIP, "gram_attention_step: %s", hipGetErrorString(e));

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
     const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int k0 = kt * kTile, wk0 = k0 + wave * 16, k = wk0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
-    const int prefix = a.prefix ? a.prefix[batch] : 0;
+    const int prefix = prefix_of(a.prefix, batch, a.length);
 
     u32x4 kf[S::KK], vf[S::KK];
     const int kseg = k < a.length ? row_segment(seg, k, a.length) : kNoSegOwner;

@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend(const AttArgs 
     const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int q0 = qt * kTile, wq0 = q0 + wave * 16, q = wq0 + c;
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
-    const int prefix = a.prefix ? a.prefix[batch] : 0;
+    const int prefix = prefix_of(a.prefix, batch, a.length);
     const T* const kp = static_cast<const T*>(a.k.data) + batch * a.k.sb + kvh * a.k.sh;
     const T* const vp = static_cast<const T*>(a.v.data) + batch * a.v.sb + kvh * a.v.sh;
 

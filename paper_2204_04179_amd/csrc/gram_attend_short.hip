@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_a
     const int c = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(wave_id());
     const int w0 = wave * 16, row = w0 + c;                     // the wave's rows, as queries and as keys
     const int* const seg = a.seg ? a.seg + (int64_t)batch * a.length : nullptr;
-    const int prefix = a.prefix ? a.prefix[batch] : 0;
+    const int prefix = prefix_of(a.prefix, batch, a.length);
     const int rseg = row < a.length ? row_segment(seg, row, a.length) : kNoSegOwner;
     const int own = rseg < 0 ? kNoSegOwner : rseg;
     const bool want_table = a.part != nullptr;

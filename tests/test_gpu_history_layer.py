@@ -292,6 +292,95 @@ def test_table_gradient_of_distances_beyond_the_near_sums(far, L, causal, both):
         lo.assert_within(got[n], want[n], n)
 
 
+def test_a_prefix_longer_than_the_history_leaves_nothing_hidden():
+    import torch
+    from paper_2204_04179_amd import gram
+    for L in (40, 150):
+        c = case("f32", 3, L, 2, 2, 16, prefix=True, docs=True, buckets=8, far=12, both=True)
+        q, k, v, do, seg, _, table = inputs(torch, c, seed=3)
+        prefix = torch.tensor([2147483647, L, -2147483648], dtype=torch.int32)
+        want = oracle_of(c, q, k, v, do, seg, prefix.clamp(0, L), table)
+        got = run_gpu(torch, gram, c, q, k, v, do, seg, prefix, table)
+        for n in got:
+            lo.assert_within(got[n], want[n], n)
+
+
+def test_strides_of_what_there_is_one_of_are_not_looked_at():
+    import torch
+    from paper_2204_04179_amd import gram
+    wild = lambda t, s: torch.as_strided(t, t.shape, s)
+    plan = gram.HistoryAttention(1, 1, 64)
+    q, k, v, do = (draw(torch, (1, 1, 1, 64), i, torch.bfloat16).cuda() for i in range(4))
+    far = (1 << 40, 1 << 40, 1 << 40, 1)
+    lse, work = torch.empty(1, 1, 1, device="cuda"), torch.empty(plan.backward_bytes(1, 1), dtype=torch.uint8, device="cuda")
+    o, dq, dk, dv = (torch.full_like(q, float("nan")) for _ in range(4))
+    plan.forward(wild(q, far), wild(k, (3, 5, 7, 1)), v, wild(o, far), lse=lse)
+    plan.backward(q, wild(k, far), v, wild(o, far), lse, do, wild(dq, far), dk, wild(dv, far), work)
+    # one key: its weight is 1 up to a few roundings of its score (2^-20 here), and so is delta dp
+    assert torch.equal(o, v) and torch.equal(dv, do) and float(dq.abs().max()) < 1e-3 and float(dk.abs().max()) < 1e-3
+
+
+@pytest.mark.parametrize("batch", [1, 120])
+def test_offsets_past_32_bits(batch):
+    """Rows 32 MiB apart (128 histories' worth of heads apart for the many): every operand reaches past 2^32 bytes, and the
+    results are those of packed operands, bit for bit."""
+    import torch
+    from paper_2204_04179_amd import gram
+    B, L, H, KV, D = batch, 150, 2, 1, 64
+    plan = gram.HistoryAttention(H, KV, D, buckets=16, max_distance=60)
+    wide = ((1 << 24) if B == 1 else (1 << 18)) + 64           # elements from row to row
+    box = torch.empty(B * L * wide, dtype=torch.bfloat16, device="cuda")
+    assert box.numel() > 1 << 31
+    heads = dict(q=H, k=KV, v=KV, o=H, do=H, dq=H, dk=KV, dv=KV)
+    far, near, at = {}, {}, 0
+    for i, (n, h) in enumerate(heads.items()):
+        near[n] = draw(torch, (B, L, h, D), i, torch.bfloat16).cuda()
+        far[n] = torch.as_strided(box, (B, L, h, D), (L * wide, wide, D, 1), at)
+        far[n].copy_(near[n])
+        at += h * D
+    table = draw(torch, (H, 16), 20, torch.float32).cuda()
+    out = []
+    for t in (near, far):
+        lse, dtable = torch.empty(B, H, L, device="cuda"), torch.empty_like(table)
+        work = torch.empty(plan.backward_bytes(B, L), dtype=torch.uint8, device="cuda")
+        plan.forward(t["q"], t["k"], t["v"], t["o"], lse=lse, table=table)
+        plan.backward(t["q"], t["k"], t["v"], t["o"], lse, t["do"], t["dq"], t["dk"], t["dv"], work, table=table, dtable=dtable)
+        so, new = torch.empty(B, H, D, dtype=torch.bfloat16, device="cuda"), near["do"][:, 0, :KV].contiguous()
+        lens = torch.full((B,), L - 1, dtype=torch.int32, device="cuda")
+        kc, vc = t["k"], t["v"]
+        plan.step(near["q"][:, 5], new, new, kc, vc, lens, so,
+                  torch.empty(plan.step_bytes(B, L), dtype=torch.uint8, device="cuda"), table=table)
+        assert torch.equal(kc[:, L - 1], new) and torch.equal(vc[:, L - 1], new)
+        out.append([lse, dtable, so] + [t[n].contiguous() for n in ("o", "dq", "dk", "dv")])
+    for a, b in zip(*out):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_longest_history(dtype):
+    """262,144 positions packed from sessions; six of them against the oracle of the session alone."""
+    import torch
+    from paper_2204_04179_amd import gram
+    L, c = 262144, case(dtype, 1, 262144, 2, 1, 16, buckets=32, far=128)
+    g = torch.Generator().manual_seed(5)
+    ends = torch.cumsum(torch.randint(1, 900, (1200,), generator=g), 0)
+    seg = torch.bucketize(torch.arange(L), ends, right=True).int()[None]
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    q, k, v, do = (draw(torch, (1, L, n, 16), i, dt) for i, n in enumerate((2, 1, 1, 2)))
+    table = draw(torch, (2, 32), 9, torch.float32)
+    got = run_gpu(torch, gram, c, q, k, v, do, seg, None, table)
+    last = int(seg[0, -1])
+    for s in (0, 1, last // 3, last // 2, last - 1, last):
+        i = torch.nonzero(seg[0] == s)[:, 0]
+        a, b = int(i[0]), int(i[-1]) + 1
+        part = [t[:, a:b] for t in (q, k, v, do)]
+        want = oracle_of({**c, "L": b - a}, *part, None, None, table)
+        for n in ("o", "dq", "dk", "dv"):
+            lo.assert_within(got[n][:, a:b], want[n], n)
+        lo.assert_within(got["lse"][:, :, a:b], want["lse"], "lse")
+    assert torch.isfinite(got["dtable"]).all()
+
+
 def test_gradients_against_differences():
     """The table's gradient and dv, dk, dq along a random direction against a central difference of the 64-bit forward."""
     import torch

@@ -87,6 +87,34 @@ def test_sizes_and_pointers_that_are_refused():
     assert lib.gram_attention_step(cfg, 0, 16, None, None, None, None, None, None, None, None, None, None, None) == gram.OK
 
 
+def test_operands_whose_written_rows_overlap_are_refused():
+    lib = gram.load()
+    plan = gram.HistoryAttention(2, 2, 8)
+    cfg, some = C.byref(plan.cfg), 1 << 20                    # never dereferenced
+    rows = lambda b=64, r=16, h=8: C.byref(gram.GramRows(some, b, r, h))
+    good, null = rows(), None
+    for bad in (rows(b=0), rows(r=0), rows(h=0), rows(h=7), rows(b=4)):
+        assert lib.gram_attention(cfg, 2, 4, good, good, good, bad, null, null, null, null, null) == gram.ERR_ARG
+        assert b"overlap" in lib.gram_last_error(None)
+        for at in range(3):
+            out = [good] * 3
+            out[at] = bad
+            assert lib.gram_attention_backward(cfg, 2, 4, good, good, good, good, some, good, *out, null, null, null, null, some,
+                                               null) == gram.ERR_ARG
+            assert b"overlap" in lib.gram_last_error(None)
+    for bad in (rows(b=0), rows(r=0), rows(h=0)):
+        for caches in ((good, bad), (bad, good)):
+            assert lib.gram_attention_step(cfg, 2, 4, good, good, good, *caches, some, null, null, good, some, null) == gram.ERR_ARG
+            assert b"overlap" in lib.gram_last_error(None)
+    # the stride of something that there is one of means nothing: only the missing pointer is to blame
+    assert lib.gram_attention(cfg, 1, 4, good, good, null, rows(b=-5), null, null, null, null, null) == gram.ERR_ARG
+    assert b"NULL" in lib.gram_last_error(None)
+    # row numbers of a cache stay below 2^30
+    assert plan.step_bytes(1, 1 << 30) > 0 and plan.step_bytes(1, (1 << 30) + 1) == 0
+    assert lib.gram_attention_step(cfg, 1, 2147483647, good, good, good, good, good, some, null, null, good, some, null) == gram.ERR_ARG
+    assert b"2^30" in lib.gram_last_error(None)
+
+
 def test_layer_norm_refusals():
     lib = gram.load()
     some = 1 << 20
