@@ -511,11 +511,14 @@ __device__ __forceinline__ void mark_tiles(TileMarks& mk, const int* __restrict_
     __syncthreads();
 }
 
-// Launches of at most as many blocks as there are CUs leave each SIMD with one wave, whose loads, products and
+// Launches of no more blocks than there are CUs leave each SIMD with one wave, whose loads, products and
 // exponentials wait for one another.  There a block takes twice the waves: SPLIT sets of four share the owner rows, each
 // walks every SPLIT-th of the tiles in LDS of its own, and the first joins what they found, always in the same order.
 // 1 x 1500 queries in 4 heads of 64: 21 us with two sets and 28 with one, gradients 56 and 73; 4 x 100 the same with both.
-constexpr int kFewBlocks = 256;
+// Up to two blocks per CU the last rows of long causal histories keep the launch waiting: 2 x 2048, 8 heads of 64, takes 34 us
+// and 42, its gradients 90 and 122 (float32: 99 and 155, 308 and 479).  Without the causal mask, whose blocks are alike, they
+// would take 143 us, and 16 x 200, 8 heads of 128, in as many blocks 16 us in place of 11.
+constexpr int kFewBlocks = 256, kLongTiles = 32;
 
 // What the second set found, handed over through LDS that held tiles (all waves behind a barrier): lane by lane.
 template <int DT> __device__ __forceinline__ void hand_over(unsigned char* room, const f32x4 (&acc)[DT], int wave, int lane)
@@ -780,6 +783,11 @@ template <typename F> inline void by_shape_and_cap(const gram_attention_config& 
 }
 inline dim3 att_grid(int items) { return dim3((unsigned)((items + 7) / 8 * 8)); }
 constexpr int att_blocks(int length, int rows) { return (length + rows - 1) / rows; }
+inline bool two_sets(const AttArgs& a)
+{
+    const int tiles = att_blocks(a.length, kTile);
+    return tiles > 1 && (a.items <= kFewBlocks || (a.causal && a.items <= 2 * kFewBlocks && tiles >= kLongTiles));
+}
 
 void attend_forward(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s);      // gram_attend_fwd.hip
 // Histories of one tile: all gradients in one launch.  False: not for this shape.

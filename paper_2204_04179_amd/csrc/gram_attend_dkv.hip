@@ -197,7 +197,7 @@ void attend_backward_keys(const gram_attention_config& c, AttArgs a, int unit, h
                 <<<att_grid(a.items), dim3(kBlock * SPLIT), 0, s>>>(a);
         };
         if constexpr (Shape<decltype(type), DP>::RB <= 256)
-            if (a.items <= kFewBlocks && a.length > kTile) return go(std::integral_constant<int, 2>{});
+            if (two_sets(a)) return go(std::integral_constant<int, 2>{});
         go(std::integral_constant<int, 1>{});
     });
 }

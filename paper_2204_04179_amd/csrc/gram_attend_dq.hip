@@ -347,7 +347,7 @@ void attend_backward_queries(const gram_attention_config& c, AttArgs a, int unit
 {
     a.items = a.batch * a.heads * att_blocks(a.length, kTile);
     a.by_tiles = FastDiv::of(att_blocks(a.length, kTile)), a.by_heads = FastDiv::of(a.heads), a.by_group = FastDiv::of(a.group);
-    const bool few = a.items <= kFewBlocks && a.length > kTile;
+    const bool few = two_sets(a);
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {
         constexpr int DP = decltype(dp)::value;
         constexpr int WAVES = Shape<decltype(type), DP>::RB <= 128 ? 3 : 2;
