@@ -185,36 +185,42 @@ template <typename T, int DP> struct Reader {
 #pragma unroll
         for (int kk = 0; kk < S::KK; ++kk) direct[kk] = c * S::RB + (((g + 4 * kk) ^ swz<T, S::NCH>(c)) * 16);
 #pragma unroll
-        for (int dt = 0; dt < S::DT; ++dt) {
-            if constexpr (sizeof(T) == 2) {
-                // group g reads rows 4 g .. 4 g + 3 of a block: lane j of it supplies row j / 4, columns 4 (j % 4) .. + 3
-                // and receives column j of the four rows
-                const int row = 4 * g + (c >> 2);
-                trans[dt] = row * S::RB + (((2 * dt + ((c & 3) >> 1)) ^ swz<T, S::NCH>(row)) * 16) + (c & 1) * 8;
-            } else {
-                trans[dt] = 4 * g * S::RB + (((4 * dt + (c >> 2)) ^ swz<T, S::NCH>(4 * g)) * 16) + (c & 3) * 4;
-            }
+        for (int dt = 0; dt < S::DT; ++dt) trans[dt] = column(lane, dt);
+    }
+    // columns 16 dt .. + 15
+    static __device__ __forceinline__ int column(int lane, int dt)
+    {
+        const int c = lane & 15, g = lane >> 4;
+        if constexpr (sizeof(T) == 2) {
+            // group g reads rows 4 g .. 4 g + 3 of a block: lane j of it supplies row j / 4, columns 4 (j % 4) .. + 3 and
+            // receives column j of the four rows
+            const int row = 4 * g + (c >> 2);
+            return row * S::RB + (((2 * dt + ((c & 3) >> 1)) ^ swz<T, S::NCH>(row)) * 16) + (c & 1) * 8;
+        } else {
+            return 4 * g * S::RB + (((4 * dt + (c >> 2)) ^ swz<T, S::NCH>(4 * g)) * 16) + (c & 3) * 4;
         }
     }
     __device__ __forceinline__ u32x4 row_frag(const unsigned char* tile, int t, int kk) const
     {
         return *reinterpret_cast<const u32x4*>(tile + t * 16 * S::RB + direct[kk]);
     }
-    // bf16: columns 16 dt .. + 15 of the 32 rows from 32 tp on, as the A operand of a product over those rows
-    __device__ __forceinline__ u32x4 col_frag2(const unsigned char* tile, int tp, int dt) const
+    // bf16: sixteen columns of the 32 rows from 32 tp on, as the A operand of a product over those rows
+    __device__ __forceinline__ u32x4 col_frag2(const unsigned char* tile, int tp, int dt) const { return column_frag2(tile, tp, trans[dt]); }
+    static __device__ __forceinline__ u32x4 column_frag2(const unsigned char* tile, int tp, int at)
     {
-        const unsigned char* p = tile + tp * 32 * S::RB + trans[dt];
+        const unsigned char* p = tile + tp * 32 * S::RB + at;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(uint32_t)(uintptr_t)p);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(uint32_t)(uintptr_t)(p + 16 * S::RB));
         return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
     // float32: the same over the 16 rows from 16 t on (row 4 g + e: the low bits of the swizzle change with e)
-    __device__ __forceinline__ u32x4 col_frag1(const unsigned char* tile, int t, int dt) const
+    __device__ __forceinline__ u32x4 col_frag1(const unsigned char* tile, int t, int dt) const { return column_frag1(tile, t, trans[dt]); }
+    static __device__ __forceinline__ u32x4 column_frag1(const unsigned char* tile, int t, int at)
     {
         u32x4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            v[e] = *reinterpret_cast<const uint32_t*>(tile + t * 16 * S::RB + e * S::RB + (trans[dt] ^ (e * 16)));
+            v[e] = *reinterpret_cast<const uint32_t*>(tile + t * 16 * S::RB + e * S::RB + (at ^ (e * 16)));
         return v;
     }
 };

@@ -22,10 +22,16 @@ template <typename T, int DP> struct ShortShared {
     float bias[2 * kTile];
     float table[kMaxBorders];
     int border[kMaxBorders];
-    float strip[kWavesPerBlock][4][kStrip];
     float bucket[kWavesPerBlock][kMaxBorders];
     float dist[kWavesPerBlock][2 * kShortDist + 1];
 };
+
+// A wave's strips of table_near lie in its own rows of the tile of weights, which are written after them.
+template <typename T> __device__ __forceinline__ float (*strips(unsigned char* weights, int wave))[kStrip]
+{
+    static_assert(4 * kStrip * sizeof(float) <= 16 * Shape<T, kTile>::RB, "four strips in sixteen rows");
+    return reinterpret_cast<float (*)[kStrip]>(weights + wave * 16 * Shape<T, kTile>::RB);
+}
 
 // Columns c of a first product (queries) as rows of a [query][key] tile.
 template <typename T> __device__ __forceinline__ void put_weights(unsigned char* tile, const f32x4 (&w)[4], int row, int g)
@@ -42,17 +48,17 @@ template <typename T> __device__ __forceinline__ void put_weights(unsigned char*
     }
 }
 
-// acc[dt] += (tile of rows)^T . (columns 16 col .. + 15 of the [query][key] tile)
+// acc[dt] += (tile of rows)^T . (sixteen columns of the [query][key] tile, which lie at `col`)
 template <typename T, int DP>
 __device__ __forceinline__ void over_queries(f32x4 (&acc)[DP / 16], const Reader<T, DP>& rd, const unsigned char* rows,
-                                             const Reader<T, kTile>& rw, const unsigned char* weights, int col)
+                                             const unsigned char* weights, int col)
 {
     constexpr int STEPS = sizeof(T) == 2 ? 2 : 4;
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
         u32x4 b;
-        if constexpr (sizeof(T) == 2) b = rw.col_frag2(weights, n, col);
-        else b = rw.col_frag1(weights, n, col);
+        if constexpr (sizeof(T) == 2) b = Reader<T, kTile>::column_frag2(weights, n, col);
+        else b = Reader<T, kTile>::column_frag1(weights, n, col);
 #pragma unroll
         for (int dt = 0; dt < DP / 16; ++dt) {
             if constexpr (sizeof(T) == 2) acc[dt] = mma<T>(rd.col_frag2(rows, n, dt), b, acc[dt]);
@@ -62,8 +68,11 @@ __device__ __forceinline__ void over_queries(f32x4 (&acc)[DP / 16], const Reader
     }
 }
 
+// Blocks per CU: LDS holds four where rows have 64 bytes, three at 128 (bf16), two or one beyond.  Registers for four are
+// worth a few spilled ones (1024 x 50, 8 heads of 32: 80 us and 86 with three) unless the cap's slopes stand in them too (2048
+// x 50: 148 us with three, 165 with four); the compiler's choice at 128 bytes beats a limit for three (74 and 87 us, heads of 64).
 template <typename T, int DP, int UNIT, bool CAP>
-__global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_attend_short(const AttArgs a)
+__global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) void k_attend_short(const AttArgs a)
 {
     using S = Shape<T, DP>;
     __shared__ ShortShared<T, DP> sh;
@@ -105,7 +114,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_a
     feed.template put<false>(sh.k, sh.v, sh.seg, masked, nullptr);
 
     const Reader<T, DP> rd(lane);
-    const Reader<T, kTile> rw(lane);
+    const int own_keys = Reader<T, kTile>::column(lane, wave);   // the wave's columns of weights
     f32x4 dk[S::DT], dv[S::DT];
 #pragma unroll
     for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -120,7 +129,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_a
         if (flat < 0 && tid < 2 * kTile - 1) sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, kTile - 1 - tid)];
         if (want_table) {
             for (int i = tid; i < kWavesPerBlock * (2 * kShortDist + 1); i += kBlock) (&sh.dist[0][0])[i] = 0.f;
-            for (int i = tid; i < kWavesPerBlock * 4 * kStrip; i += kBlock) (&sh.strip[0][0][0])[i] = 0.f;
+            for (int i = lane; i < 4 * kStrip; i += kWave) strips<T>(sh.w, wave)[0][i] = 0.f;
             if (tid < kMaxBorders)
                 for (int w = 0; w < kWavesPerBlock; ++w) sh.bucket[w][tid] = 0.f;
         }
@@ -163,7 +172,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_a
                 for (int n = 0; n < 4; ++n) sum += (dp[n][0] + dp[n][1]) + (dp[n][2] + dp[n][3]);
                 add_bucket(sh.bucket[wave], flat, sum, lane);
             } else {
-                table_near(a, dp, w0, sh.strip[wave], &sh.dist[wave][kShortDist], sh.bucket[wave], sh.border, lane);
+                table_near(a, dp, w0, strips<T>(sh.w, wave), &sh.dist[wave][kShortDist], sh.bucket[wave], sh.border, lane);
             }
         }
         if constexpr (CAP) {
@@ -177,8 +186,8 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_a
         for (int dt = 0; dt < S::DT; ++dt) dq[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         second_product<T, DP>(dq, dp, rd, sh.k);
         __syncthreads();
-        over_queries<T, DP>(dv, rd, sh.d, rw, sh.w, wave);
-        over_queries<T, DP>(dk, rd, sh.q, rw, sh.dz, wave);
+        over_queries<T, DP>(dv, rd, sh.d, sh.w, own_keys);
+        over_queries<T, DP>(dk, rd, sh.q, sh.dz, own_keys);
         if (want_table) {
             const float* const at0 = &sh.dist[0][kShortDist];
             constexpr int W = 2 * kShortDist + 1;
