@@ -22,8 +22,15 @@ __global__ __launch_bounds__(1024) void k_attend_dtable(const float* __restrict_
     }
     s[threadIdx.x] = sum;
     __syncthreads();
+    if (strand < 8) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) sum += s[k * 128 + threadIdx.x];
+        s[threadIdx.x] = sum;
+    }
+    __syncthreads();
     if (strand == 0 && b < buckets) {
-        for (int k = 1; k < 64; ++k) sum += s[k * 16 + threadIdx.x];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) sum += s[k * 16 + threadIdx.x];
         dtable[(int64_t)head * buckets + b] = (float)sum;
     }
 }
