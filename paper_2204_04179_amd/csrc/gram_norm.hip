@@ -14,7 +14,8 @@ namespace gram {
 namespace {
 
 constexpr int kNormMaxParts = 1024;     // blocks of the backward pass: four per CU, each with its partial dw and db
-constexpr int kNormPartRows = 16;       // rows per block at least
+constexpr int kNormPartRows = 16;       // rows per block at least,
+constexpr int kNormWideRows = 4;        // where a block takes one row at a time
 
 typedef float nf32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t nu32x2 __attribute__((ext_vector_type(2)));
@@ -314,15 +315,16 @@ __global__ __launch_bounds__(1024) void k_layer_norm_parts(const float* __restri
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-int norm_parts(int64_t m)
+int norm_parts(int64_t m, int rows)
 {
-    const int64_t p = (m + kNormPartRows - 1) / kNormPartRows;
+    const int64_t p = (m + rows - 1) / rows;
     return (int)(p > kNormMaxParts ? kNormMaxParts : p);
 }
 
 // Lanes per row and chunks per lane by the width: the narrowest group of lanes that holds a row in registers (a row of
-// 32 columns in a whole wave would leave 60 lanes without work).  `vec` columns travel per load: 16 bytes of bf16 where
-// width and addresses allow it.
+// 32 columns in a whole wave would leave 60 lanes without work; 1001 in the 32 chunks of a block that the widest rows need
+// took five times as long as in 16 chunks of a wave).  `vec` columns travel per load: 16 bytes of bf16 where width and addresses
+// allow it.  Blocks, and with them parts, of one row at a time only beyond 512 columns (gram_layer_norm_work_bytes).
 template <typename F> bool norm_shape(int vec, int d, F&& go)
 {
 #define GRAM_NORM(V, C, L) return go(std::integral_constant<int, V>{}, std::integral_constant<int, C>{}, std::integral_constant<int, L>{})
@@ -337,10 +339,13 @@ template <typename F> bool norm_shape(int vec, int d, F&& go)
         if (d <= 64) GRAM_NORM(4, 1, 16);
         if (d <= 256) GRAM_NORM(4, 1, 64);
         if (d <= 1024) GRAM_NORM(4, 4, 64);
+        if (d <= 2048) GRAM_NORM(4, 8, 64);
         GRAM_NORM(4, 8, 256);
     }
     if (d <= 64) GRAM_NORM(1, 4, 16);
     if (d <= 512) GRAM_NORM(1, 8, 64);
+    if (d <= 1024) GRAM_NORM(1, 16, 64);
+    if (d <= 2048) GRAM_NORM(1, 8, 256);
     GRAM_NORM(1, 32, 256);
 #undef GRAM_NORM
 }
@@ -371,7 +376,8 @@ extern "C" {
 int64_t gram_layer_norm_work_bytes(int64_t m, int32_t d)
 {
     if (norm_args(m, d, GRAM_F32, GRAM_F32)) return 0;
-    return (int64_t)(norm_parts(m) > 0 ? norm_parts(m) : 1) * 2 * d * (int64_t)sizeof(float);
+    const int parts = norm_parts(m, d > 512 ? kNormWideRows : kNormPartRows);    // of any alignment
+    return (int64_t)(parts > 0 ? parts : 1) * 2 * d * (int64_t)sizeof(float);
 }
 
 int gram_layer_norm(const void* x, int32_t x_dtype, const float* weight, const float* bias, const int32_t* segments,
@@ -410,7 +416,7 @@ int gram_layer_norm_backward(const void* x, int32_t x_dtype, const float* weight
     if ((reinterpret_cast<uintptr_t>(work) & 3) != 0)
         return fail_call(GRAM_ERR_ARG, "gram_layer_norm_backward: work must be 4-byte aligned");
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int parts = norm_parts(m);
+    int parts = 0;
     float* const part = static_cast<float*>(work);
     if (m > 0) {
         const bool al = aligned16(x) && aligned16(weight) && aligned16(dy) && aligned16(dx) && (!add || aligned16(add));
@@ -419,6 +425,7 @@ int gram_layer_norm_backward(const void* x, int32_t x_dtype, const float* weight
             return norm_shape(vec, d, [&](auto V, auto C, auto L) {
                 using TX = std::remove_pointer_t<decltype(tx)>;
                 using TY = std::remove_pointer_t<decltype(ty)>;
+                parts = norm_parts(m, decltype(L)::value == 256 ? kNormWideRows : kNormPartRows);
                 k_layer_norm_bwd<TX, TY, decltype(V)::value, decltype(C)::value, decltype(L)::value>
                     <<<dim3((unsigned)parts), dim3(kBlock), 0, s>>>(static_cast<const TX*>(x), weight, stats,
                                                                     static_cast<const TY*>(dy), segments, add, m, d,

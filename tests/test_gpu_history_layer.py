@@ -53,6 +53,13 @@ def test_layer_norm_and_its_backward(M, d, xt, yt, padded):
     lo.assert_within(plain, lo.layer_norm(x, w, b, t[yt], seg, dy=dy)["dx"], "dx without add")
 
 
+@pytest.mark.parametrize("M,d,xt,yt,padded", [(300, 513, "bf16", "bf16", True), (3001, 1001, "bf16", "f32", False), (35, 1023, "f32", "bf16", False),
+                                              (9, 1025, "f32", "f32", True), (5003, 1499, "bf16", "bf16", False), (6, 2047, "f32", "bf16", False),
+                                              (70, 1500, "bf16", "bf16", True), (21, 2044, "f32", "f32", False), (13, 2049, "bf16", "bf16", True)])
+def test_layer_norm_of_wide_rows_of_any_alignment(M, d, xt, yt, padded):
+    test_layer_norm_and_its_backward(M, d, xt, yt, padded)
+
+
 # ---- attention --------------------------------------------------------------------------------------------
 
 
