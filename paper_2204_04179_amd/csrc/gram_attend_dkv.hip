@@ -1,6 +1,10 @@
 // Attention over item histories, backward pass over the keys (notation of gram_attend_fwd.hip and gram_attend_dq.hip):
 //
 //   dk_j = scale sum_i dz_ij q_i       dv_j = sum_i p_ij do_i       over the queries of every head that shares the key
+//
+// 1024 x 200 positions, 8 heads of 128, causal, bf16: 1.15 ms.  A block's own keys and values and its stores alone take 0.36 of
+// it, as long as the memory needs; with two waves per SIMD (the accumulators of dk and dv are 64 registers, 253 in all) little of
+// the staging and of the products hides behind the other.
 #include "gram_attend.h"
 
 namespace gram {

@@ -4,9 +4,11 @@
 //   dp_ij = do_i.v_j   delta_i = sum_j p_ij dp_ij   ds_ij = p_ij (dp_ij - delta_i)   dz_ij = ds_ij (1 - (c_ij / cap)^2)
 //   dq_i = scale sum_j dz_ij k_j       dtable[head, b] = sum of ds over the pairs of bucket b
 //
-// delta is do.o where only dq, dk and dv are asked for, whose own rounding is as coarse as that of o.  The table's gradient
-// is float32, sums over whole batches in which an error of delta does not average out: for it a first walk over the keys
-// sums p dp in float32.
+// delta is summed in float32 from the weights, not do.o, which knows o to as many bits as it was stored in: the table's
+// gradient is a sum over whole batches in which an error of delta does not average out.  (float32 without a table takes do.o.)
+//
+// 1024 x 200 positions, 8 heads of 128, causal, bf16: 1.02 ms with the table's gradient, 0.6 without; 0.45 would move q, k, v, do and
+// dq once.  Registers allow two waves per SIMD, which wait half of the time.
 #include "gram_attend.h"
 
 namespace gram {

@@ -5,6 +5,9 @@
 //   o_i = sum_j p_ij v_j,  p_ij = exp(s_ij - lse_i) over the visible j
 //
 // One pass over the keys with the running maximum and sum of the softmax; scores and weights stay in registers.
+//
+// 1024 x 200 positions, 8 heads of 128, causal, a table, bf16: 0.54 ms, where reading q, k, v and writing o would take 0.36 at a
+// large copy's rate.  Half of a wave's life is waiting (barriers and LDS, three waves per SIMD), a fifth vector arithmetic.
 #include "gram_attend.h"
 
 namespace gram {

@@ -4,6 +4,9 @@
 // A block takes one history and key head: queries, keys, values and dout of a head lie in LDS as one tile each, scores and
 // weights are worked out once (the passes of longer histories do so up to three times), by waves that own 16 queries; the
 // weights and their gradients then change hands through LDS to waves that own 16 keys.  delta comes from the tile itself.
+//
+// 128 x 55, 20 heads of 20, bf16, a table: 30 us, 34 MB at 1.1 TB/s; bound by one tile's chain of loads, products and exchanges,
+// which up to four blocks per CU overlap.  1024 x 50, 4 heads of 64: 74 us, of that the table's gradient 22.
 #include "gram_attend.h"
 
 namespace gram {
