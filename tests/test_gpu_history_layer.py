@@ -60,6 +60,46 @@ def test_layer_norm_of_wide_rows_of_any_alignment(M, d, xt, yt, padded):
     test_layer_norm_and_its_backward(M, d, xt, yt, padded)
 
 
+@pytest.mark.parametrize("M,d", [(300, 32), (257, 400), (130, 1001), (70, 4096)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layer_norm_in_place(M, d, dtype):
+    """y may be x, and dx the gradient that is added to it: the same bits as apart."""
+    import torch
+    from paper_2204_04179_amd import gram
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    x, dy, past = draw(torch, (M, d), 1, t, 1.5).cuda(), draw(torch, (M, d), 2, t).cuda(), draw(torch, (M, d), 3, torch.float32).cuda()
+    w, b = draw(torch, (d,), 4, torch.float32).cuda(), draw(torch, (d,), 5, torch.float32).cuda()
+    y, stats, twice = torch.empty_like(x), torch.empty(M, 2, device="cuda"), x.clone()
+    gram.layer_norm(x, w, b, y, stats=stats)
+    gram.layer_norm(twice, w, b, twice)
+    dx, dw, db, same = torch.empty_like(past), torch.empty(d, device="cuda"), torch.empty(d, device="cuda"), past.clone()
+    work = torch.empty(gram.layer_norm_work_bytes(M, d), dtype=torch.uint8, device="cuda")
+    gram.layer_norm_backward(x, w, stats, dy, dx, dw, db, work, add=past)
+    gram.layer_norm_backward(x, w, stats, dy, same, dw, db, work, add=same)
+    assert torch.equal(twice, y) and torch.equal(same, dx)
+
+
+def test_empty_batches():
+    import torch
+    from paper_2204_04179_amd import gram
+    e = lambda *s, dt=torch.float32: torch.empty(*s, dtype=dt, device="cuda")
+    w, dw, db = torch.ones(24, device="cuda"), torch.ones(24, device="cuda"), torch.ones(24, device="cuda")
+    x, work = e(0, 24), e(gram.layer_norm_work_bytes(0, 24), dt=torch.uint8)
+    gram.layer_norm(x, w, w, x)
+    gram.layer_norm_backward(x, w, e(0, 2), x, x, dw, db, work)
+    assert not dw.any() and not db.any()
+    plan = gram.HistoryAttention(2, 1, 8, dtype=gram.F32, buckets=4, max_distance=9)
+    table = torch.ones(2, 4, device="cuda")
+    for B, L in ((0, 5), (3, 0)):
+        dtable = torch.ones(2, 4, device="cuda")
+        q, k, lse, work = e(B, L, 2, 8), e(B, L, 1, 8), e(B, 2, L), e(plan.backward_bytes(B, L), dt=torch.uint8)
+        plan.forward(q, k, k, q, lse=lse, table=table)
+        plan.backward(q, k, k, q, lse, q, q, k, k, work, table=table, dtable=dtable)
+        assert not dtable.any()
+    plan.step(e(0, 2, 8), e(0, 1, 8), e(0, 1, 8), e(0, 6, 1, 8), e(0, 6, 1, 8), e(0, dt=torch.int32), e(0, 2, 8),
+              e(plan.step_bytes(0, 6), dt=torch.uint8), table=table)
+
+
 # ---- attention --------------------------------------------------------------------------------------------
 
 
@@ -361,6 +401,27 @@ def test_offsets_past_32_bits(batch):
         out.append([lse, dtable, so] + [t[n].contiguous() for n in ("o", "dq", "dk", "dv")])
     for a, b in zip(*out):
         assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_heads_of_a_long_causal_history_are_what_each_is_alone(dtype):
+    """9 x 32 blocks of 64 rows, and 32 for a head of its own: the same bits, and one of the heads against the oracle."""
+    import torch
+    from paper_2204_04179_amd import gram
+    c = case(dtype, 1, 2048, 9, 9, 24, buckets=16, far=300)
+    q, k, v, do, _, _, table = inputs(torch, c, seed=11)
+    every = run_gpu(torch, gram, c, q, k, v, do, None, None, table)
+    one = {**c, "H": 1, "KV": 1}
+    for h in (0, 4, 8):
+        part = [t[:, :, h:h + 1] for t in (q, k, v, do)]
+        alone = run_gpu(torch, gram, one, *part, None, None, table[h:h + 1])
+        for n in ("o", "dq", "dk", "dv"):
+            assert torch.equal(every[n][:, :, h:h + 1], alone[n]), (n, h)
+        assert torch.equal(every["lse"][:, h:h + 1], alone["lse"]) and torch.equal(every["dtable"][h:h + 1], alone["dtable"])
+        if h == 4:
+            want = oracle_of(one, *part, None, None, table[h:h + 1])
+            for n in alone:
+                lo.assert_within(alone[n], want[n], n)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
