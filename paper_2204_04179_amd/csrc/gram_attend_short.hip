@@ -232,7 +232,9 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
 
 bool attend_backward_short(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s)
 {
-    // four tiles of rows and two of weights have to fit a CU's LDS: float32 rows of more than 64 elements do not
+    // four tiles of rows and two of weights have to fit a CU's LDS: float32 rows of more than 64 elements do not.  Against a launch
+    // for the queries and one for the keys: 64 x 50, 4 heads of 128, 17 us and 22; 1024 x 60, 4 heads of 64 in float32, 205 and 221;
+    // 1024 x 50, 4 heads of 128, 142 and 145, but with the table's gradient 180 and 164.
     if (a.length > kTile || (c.dtype == GRAM_F32 && c.head_dim > 64)) return false;
     a.items = a.batch * a.kv_heads;
     a.by_heads = FastDiv::of(a.kv_heads);
