@@ -143,7 +143,8 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
             for (int n = 0; n < 4; ++n) s[n] -= *reinterpret_cast<const f32x4*>(&sh.lse[16 * n + 4 * g]);
             if (!whole(t, wk0 + 15, mixed)) {
                 if (sh.bad[parity][0] | sh.bad[parity][1]) spoil_rows(s, sh.bad[parity], g);
-                if (mixed) mask_scores<true, true>(s, sh.seg, own, first - q0, lane);
+                // rows past the history's end are no one's segment; without weight, whatever their bias is
+                if (mixed || q0 + kTile > a.length) mask_scores<true, true>(s, sh.seg, own, first - q0, lane);
                 else mask_scores<false, true>(s, sh.seg, own, first - q0, lane);
             }
 #pragma unroll
