@@ -141,8 +141,9 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
             if (flat < 0) add_bias(s, &sh.bias[4 * g - (k - k0) + kTile - 1]);
 #pragma unroll
             for (int n = 0; n < 4; ++n) s[n] -= *reinterpret_cast<const f32x4*>(&sh.lse[16 * n + 4 * g]);
+            // rows are marked for the block: also where this wave's keys are visible to the whole tile
+            if (masked && (sh.bad[parity][0] | sh.bad[parity][1])) spoil_rows(s, sh.bad[parity], g);
             if (!whole(t, wk0 + 15, mixed)) {
-                if (sh.bad[parity][0] | sh.bad[parity][1]) spoil_rows(s, sh.bad[parity], g);
                 // rows past the history's end are no one's segment; without weight, whatever their bias is
                 if (mixed || q0 + kTile > a.length) mask_scores<true, true>(s, sh.seg, own, first - q0, lane);
                 else mask_scores<false, true>(s, sh.seg, own, first - q0, lane);

@@ -43,3 +43,59 @@ def test_an_entry_of_the_table_that_no_pair_reaches_changes_nothing(dtype):
     got = run_gpu(torch, gram, c, *data, table)
     for n in got:
         lo.assert_within(got[n], want[n], n)
+
+
+# ---- values that are not finite ---------------------------------------------------------------------------
+
+
+def check_spoilt(c, at, what, odd, prefix=None, segments=None):
+    """Position `at` of every history holds the value `odd` in the operand `what` (or in all).  Rows that have nothing to do
+    with it are what the definition has for them; every gradient that it enters is not finite in any head."""
+    import torch
+    from paper_2204_04179_amd import gram
+    q, k, v, do, _, _, table = inputs(torch, c, seed=100)
+    B, L = c["B"], c["L"]
+    pre = None if prefix is None else torch.tensor([prefix[b % len(prefix)] for b in range(B)], dtype=torch.int32)
+    seg = None if segments is None else torch.full((B, L), segments, dtype=torch.int32)
+    clean = [t.clone() for t in (q, k, v, do)]
+    for n, t, z in zip(("q", "k", "v", "do"), (q, k, v, do), clean):
+        if what in (n, "all"):
+            t[:, at], z[:, at] = odd, 0.0
+    bad = torch.zeros(B, L, dtype=torch.bool)
+    bad[:, at] = True
+    want = oracle_of(c, *clean, seg, pre, table)
+    got = {n: t.cpu() for n, t in run_gpu(torch, gram, c, q, k, v, do, seg, pre, table).items()}
+    see = lo.visible(L, seg, c["causal"], pre, B)[:, 0].expand(B, L, L)               # [B, query, key]
+    held = bad if what in ("k", "v", "all") else torch.zeros_like(bad)
+    row = (see & held[:, None, :]).any(2) | (bad if what in ("q", "all") else False)   # queries without a result
+    grow = row | (bad if what == "do" else False)                                     # and without gradients
+    gkey = (see & grow[:, :, None]).any(1)                                            # keys that those see
+    for n, spoilt in (("o", row), ("dq", grow), ("dk", gkey), ("dv", gkey)):
+        value, bound = want[n]
+        lo.assert_within(got[n][~spoilt], (value[~spoilt], bound[~spoilt]), f"{n} of the others")
+        if (n, what) != ("dv", "v"):                       # dv is made of weights and do: a value has no part in it
+            finite = torch.isfinite(got[n][spoilt].float()).all(-1)
+            assert not bool(finite.any()), f"{n}: {int(finite.sum())} of {finite.numel()} rows and heads are finite"
+    if table is not None:
+        i = torch.arange(L)
+        of = lo.buckets_of(i[:, None] - i[None, :], c["buckets"], c["far"], c["both"])
+        reached = torch.zeros(c["buckets"], dtype=torch.bool)
+        reached[of[(see & grow[:, :, None]).any(0)]] = True
+        assert not bool(torch.isfinite(got["dtable"][:, reached]).any()), "dtable"
+
+
+# A prefix that ends within a tile: some waves of a block see all of a tile and others do not.
+INSIDE = [
+    (case("bf16", 1, 200, 2, 1, 64, prefix=True), (40,), 20), (case("bf16", 1, 200, 2, 1, 64, prefix=True), (40,), 50),
+    (case("f32", 2, 200, 2, 2, 20, prefix=True, buckets=8, far=30, both=True), (100, 40), 33),
+    (case("bf16", 70, 130, 2, 2, 128, prefix=True), (100, 40, 127), 70),
+    (case("f32", 1, 300, 4, 2, 128, prefix=True, cap=5.0), (100,), 110),
+]
+
+
+@pytest.mark.parametrize("what", ["k", "v", "q", "do", "all"])
+@pytest.mark.parametrize("c,prefix,at", INSIDE, ids=lambda p: name_of(p) if isinstance(p, dict) else str(p))
+def test_non_finite_values_where_a_prefix_ends_within_a_tile(c, prefix, at, what):
+    check_spoilt(c, at, what, float("nan"), prefix=prefix)
+    if what in ("do", "v"):
+        check_spoilt(c, at, what, float("inf"), prefix=prefix)
