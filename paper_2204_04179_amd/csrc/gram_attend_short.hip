@@ -99,7 +99,6 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
         last = last < a.length ? last : a.length;
     }
     if (row >= a.length) last = 0;
-    const bool masked = seg || a.causal || a.length < kTile;
     const int flat = a.bk.side ? uniform_bucket(a.bk, 1 - kTile, kTile - 1) : 0;
 
     Feed<T, DP, UNIT> feed(tid);
@@ -114,6 +113,10 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
         lse_ahead = a.lse[((int64_t)batch * a.heads + head) * a.length + (row < a.length ? row : a.length - 1)];
     };
     load_queries(0);
+    // whether any pair is masked, by the forward pass's rule: where none is, it has left non-finite values of k and v in place and
+    // what they reach is not finite; elsewhere they are zeros here, and the rows that see them have NaN for their lse
+    const int one = __builtin_amdgcn_readfirstlane(feed.seg);
+    const bool masked = one == kNoSeg || !__all(feed.seg == one) || (a.causal && prefix < kTile);
     feed.template put<false>(sh.k, sh.v, sh.seg, masked, nullptr);
 
     const Reader<T, DP> rd(lane);

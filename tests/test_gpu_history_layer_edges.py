@@ -99,3 +99,19 @@ def test_non_finite_values_where_a_prefix_ends_within_a_tile(c, prefix, at, what
     check_spoilt(c, at, what, float("nan"), prefix=prefix)
     if what in ("do", "v"):
         check_spoilt(c, at, what, float("inf"), prefix=prefix)
+
+
+# One whole tile, all of it visible: no padding, one session or none, every position within the prefix.
+WHOLE = [
+    (case("bf16", 2, 64, 2, 1, 64, causal=False, buckets=8, far=30, both=True), None, 0),
+    (case("f32", 2, 64, 2, 2, 20, causal=False), None, 7), (case("bf16", 3, 64, 2, 2, 128, prefix=True, buckets=8, far=30), (64, 90), None),
+    (case("f32", 1, 64, 4, 2, 64, prefix=True, cap=5.0), (64,), 2), (case("bf16", 2, 64, 2, 2, 32, prefix=True), (64, 63, 20), 1),
+]
+
+
+@pytest.mark.parametrize("what", ["k", "v", "q", "do", "all"])
+@pytest.mark.parametrize("c,prefix,segments", WHOLE, ids=lambda p: name_of(p) if isinstance(p, dict) else str(p))
+def test_non_finite_values_in_a_history_of_one_whole_tile(c, prefix, segments, what):
+    check_spoilt(c, 10, what, float("nan"), prefix=prefix, segments=segments)
+    if what in ("do", "v"):
+        check_spoilt(c, 10, what, float("inf"), prefix=prefix, segments=segments)
