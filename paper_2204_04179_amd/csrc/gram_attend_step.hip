@@ -28,6 +28,9 @@ struct StepArgs {
     AttBuckets bk;
 };
 
+// Zero where nothing was seen (an idle history) or only scores of minus infinity.
+__device__ __forceinline__ float step_result(float x, float top, float sum) { return top == -INFINITY && sum == 0.f ? x * 0.f : x / sum; }
+
 template <typename T, int DP, int UNIT>
 __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_step(const StepArgs a)
 {
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_s
         const int head = head0 + h;
         if (a.splits == 1) {
             T* const op = static_cast<T*>(a.o.data) + b * a.o.sb + head * a.o.sh + d;
-            const float r = rows == 0 ? 0.f : x / sum;
+            const float r = step_result(x, mx, sum);
             if constexpr (sizeof(T) == 2) op->bits = (uint16_t)pack_bf16x2(r, 0.f);
             else *op = r;
         } else {
@@ -265,8 +268,7 @@ template <typename T> __global__ __launch_bounds__(128) void k_step_join(const S
         sum += ps[a.dim + 1] * f;
         x += ps[d] * f;
     }
-    const int n = a.lengths[b];
-    const float r = n >= 0 && n < a.capacity ? x / sum : 0.f;
+    const float r = step_result(x, mx, sum);
     T* const op = static_cast<T*>(a.o.data) + b * a.o.sb + head * a.o.sh + d;
     if constexpr (sizeof(T) == 2) op->bits = (uint16_t)pack_bf16x2(r, 0.f);
     else *op = r;

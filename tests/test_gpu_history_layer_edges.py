@@ -115,3 +115,31 @@ def test_non_finite_values_in_a_history_of_one_whole_tile(c, prefix, segments, w
     check_spoilt(c, 10, what, float("nan"), prefix=prefix, segments=segments)
     if what in ("do", "v"):
         check_spoilt(c, 10, what, float("inf"), prefix=prefix, segments=segments)
+
+
+# ---- scores of minus infinity, biases far from zero -------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_step_whose_scores_are_all_minus_infinity_yields_zeros(dtype):
+    """As in the forward pass.  Caches of one part and of several; histories that see other rows too are not touched by it."""
+    import torch
+    from paper_2204_04179_amd import gram
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    for rows, lens in ((7, [0, 3, -1, 6]), (1500, [0, 1499, 1500, 700])):
+        lens = torch.tensor(lens, dtype=torch.int32)
+        q, kn, vn = draw(torch, (4, 2, 16), 1, dt), draw(torch, (4, 1, 16), 2, dt), draw(torch, (4, 1, 16), 3, dt)
+        kc, vc = draw(torch, (4, rows, 1, 16), 4, dt), draw(torch, (4, rows, 1, 16), 5, dt)
+        for hidden in (1, 8):                              # the new item alone; everything
+            table = draw(torch, (2, 8), 6, torch.float32)
+            table[:, :hidden] = -float("inf")
+            seen = table.clone()
+            seen[:, :hidden] = -200.0                      # exp(-200) is nothing beside the others
+            o, bound, _, _ = lo.step(q, kn, vn, kc, vc, lens, scale=0.25, table=seen, far=20)
+            nothing = torch.tensor([n == 0 or hidden == 8 for n in lens.tolist()])
+            o[nothing], bound[nothing] = 0.0, 0.0
+            plan = gram.HistoryAttention(2, 1, 16, dtype=gram.F32 if dtype == "f32" else gram.BF16, buckets=8, max_distance=20)
+            O = torch.full((4, 2, 16), float("nan"), dtype=dt, device="cuda")
+            work = torch.empty(plan.step_bytes(4, rows), dtype=torch.uint8, device="cuda")
+            plan.step(q.cuda(), kn.cuda(), vn.cuda(), kc.cuda(), vc.cuda(), lens.cuda(), O, work, table=table.cuda())
+            lo.assert_within(O, (o, bound), f"o of {rows}, {hidden} hidden")
