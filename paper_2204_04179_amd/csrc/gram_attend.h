@@ -68,6 +68,7 @@ struct AttArgs {
     const float* table;
     float* lse;
     float* delta;            // [batch, heads, length]
+    float* far;              // [batch, heads, length, 2]: maximum and log2 of the sum of rows whose lse is far from zero
     float* part;             // partial gradients of the table: [heads, parts, buckets]
     int batch, length, heads, kv_heads, group, dim;
     int causal;
@@ -374,14 +375,21 @@ __device__ __forceinline__ float tanh_f32(float x)
     return fabsf(x) < 0.4f ? s : far;
 }
 
+// An entry of the table in units of log 2, rounded by itself wherever it is used, so that a pair has the same score in every pass.
+__device__ __forceinline__ float table_log2(float entry)
+{
+#pragma clang fp contract(off)
+    return entry * kLog2e;
+}
+
 // A tile's products to scores in units of log 2: scaled, capped, with the bias `flat2` of the whole tile; slope (capped
 // scores only): d score / d product over the scale.  The groups are kept apart, or the compiler works on all 16 at once and runs
 // out of registers.
-template <bool CAP>
-__device__ __forceinline__ void to_scores(f32x4 (&s)[4], f32x4 (&slope)[CAP ? 4 : 1], float zc, float cap2, float z2, float flat2)
+template <bool CAP, int N>
+__device__ __forceinline__ void to_scores(f32x4 (&s)[N], f32x4 (&slope)[CAP ? N : 1], float zc, float cap2, float z2, float flat2)
 {
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
+    for (int n = 0; n < N; ++n) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             if constexpr (CAP) {
@@ -428,6 +436,12 @@ __device__ __forceinline__ int uniform_bucket(const AttBuckets& bk, int lo, int 
     if (hi < 0 && -hi >= bk.last) return 2 * bk.side - 1;
     return -1;
 }
+
+// The backward pass has 2^(s - lse) for weights, and lse is one float32: far from zero the log of a row's sum is lost beside its
+// largest score, and the rounding alone is a factor (a power of two and more from 1e8 on, where programs mask with a
+// bias).  Rows beyond this |lse| are given their maximum and sum again, as two numbers; up to it a weight is off by less than 2^-15.
+constexpr float kFarLse = 256.f;
+__device__ __forceinline__ bool far_lse(float lse) { return fabsf(lse) > kFarLse && fabsf(lse) < INFINITY; }
 
 // ---- non-finite values ------------------------------------------------------------------------------------
 //
@@ -619,9 +633,9 @@ template <typename T, int DP, int UNIT> struct Feed {
 };
 
 // A tile's masked scores: minus infinity where the row of the tile is not in the owner's segment (SEGMENTS; else only the
-// place counts) or not below `edge` (FROM: from `edge` on).
+// place counts) or not below `edge` (FROM: among the `span` rows from `edge` on).
 template <bool SEGMENTS, bool FROM>
-__device__ __forceinline__ void mask_scores(f32x4 (&s)[4], const int* s_seg, int own, int edge, int lane)
+__device__ __forceinline__ void mask_scores(f32x4 (&s)[4], const int* s_seg, int own, int edge, int lane, int span = 0)
 {
     const int g4 = 4 * (lane >> 4);
 #pragma unroll
@@ -631,7 +645,8 @@ __device__ __forceinline__ void mask_scores(f32x4 (&s)[4], const int* s_seg, int
         if (SEGMENTS) sg = *reinterpret_cast<const i32x4*>(s_seg + 16 * n + g4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const bool see = (!SEGMENTS || sg[r] == own) && (FROM ? 16 * n + r >= edge - g4 : 16 * n + r < edge - g4);
+            const bool in = FROM ? (uint32_t)(16 * n + r + (g4 - edge)) < (uint32_t)span : 16 * n + r < edge - g4;
+            const bool see = (!SEGMENTS || sg[r] == own) && in;
             s[n][r] = see ? s[n][r] : -INFINITY;
         }
     }

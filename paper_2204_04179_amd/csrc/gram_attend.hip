@@ -191,7 +191,7 @@ int64_t gram_attention_backward_bytes(const gram_attention_config* cfg, int32_t 
 {
     if (check_sizes(cfg, batch, length)) return 0;
     const int64_t rows = (int64_t)batch * cfg->heads;
-    return up256(rows * length * (int64_t)sizeof(float)) +
+    return up256(rows * length * (int64_t)sizeof(float)) + up256(rows * length * 2 * (int64_t)sizeof(float)) +
            up256(rows * att_blocks(length, 64) * cfg->buckets * (int64_t)sizeof(float)) + 256;
 }
 
@@ -221,14 +221,15 @@ int gram_attention_backward(const gram_attention_config* cfg, int32_t batch, int
             return fail_call(GRAM_ERR_ARG, "gram_attention_backward: work must be 16-byte aligned");
         fill(a, *cfg, batch, length);
         a.seg = segments, a.prefix = prefix, a.table = table, a.lse = const_cast<float*>(lse);
-        a.delta = static_cast<float*>(work);
-        a.part = dtable ? reinterpret_cast<float*>(static_cast<unsigned char*>(work) +
-                                                   up256((int64_t)batch * cfg->heads * length * (int64_t)sizeof(float)))
-                        : nullptr;
+        const int64_t rows = (int64_t)batch * cfg->heads * length;
+        unsigned char* at = static_cast<unsigned char*>(work);
+        a.delta = reinterpret_cast<float*>(at), at += up256(rows * (int64_t)sizeof(float));
+        a.far = reinterpret_cast<float*>(at), at += up256(rows * 2 * (int64_t)sizeof(float));
+        a.part = dtable ? reinterpret_cast<float*>(at) : nullptr;
         a.parts = batch * att_blocks(length, kTile);
         const int unit = u.unit();
         if (!attend_backward_short(*cfg, a, unit, s)) {
-            attend_backward_queries(*cfg, a, unit, s);  // also leaves delta for the pass over the keys
+            attend_backward_queries(*cfg, a, unit, s);  // also leaves delta and far for the pass over the keys
             attend_backward_keys(*cfg, a, unit, s);
         }
     }

@@ -14,7 +14,7 @@ namespace {
 template <typename T, int DP> struct DkvShared {
     __attribute__((aligned(1024))) unsigned char q[Shape<T, DP>::TILE], d[Shape<T, DP>::TILE];
     __attribute__((aligned(16))) int seg[kTile];
-    __attribute__((aligned(16))) float lse[kTile], delta[kTile];
+    __attribute__((aligned(16))) float less[kTile], delta[kTile], low[kTile];       // weights are 2^(s - less - low)
     uint32_t bad[2][2];                            // rows of a tile (by parity) that are marked
     float bias[2 * kTile];
     int border[kMaxBorders];
@@ -71,7 +71,8 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
     Feed<T, DP, UNIT> feed(tid);
     float row_lse = 0.f, row_delta = 0.f;
     const float z2 = a.scale * kLog2e, zc = CAP ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
-    const int first = a.causal && k >= prefix ? k : 0;            // queries from it on see the key, segments aside
+    int first = a.causal && k >= prefix ? k : 0;                  // queries from it to the history's end see the key, segments aside
+    first = first < a.length ? first : a.length;
     // whether all pairs of the query tile with keys up to `row` are visible
     auto whole = [&](int t, int row, bool mixed) {
         const int q0 = t * kTile;
@@ -113,21 +114,31 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
         const float* const table = a.table + (int64_t)(kvh * a.group + h) * buckets;
         __syncthreads();
         const bool masked = !whole(t, k0 + kTile - 1, mixed);
+        bool far = false;                                     // some row of the tile is
         if (there) {
             feed.template put<false>(sh.q, sh.d, sh.seg, masked, sh.bad[parity]);
+            far = __any(feed.seg != kNoSeg && far_lse(row_lse));
             if (wave == 0) {
                 // a query whose statistics are not finite sees a non-finite value; it is marked like one that holds it
-                float lse2 = row_lse == -INFINITY || feed.seg == kNoSeg ? 0.f : row_lse * kLog2e, dl = feed.seg == kNoSeg ? 0.f : row_delta;
-                if (masked && (!(fabsf(lse2) < INFINITY) || !(fabsf(dl) < INFINITY))) {
-                    lse2 = dl = 0.f;
+                float less = row_lse == -INFINITY || feed.seg == kNoSeg ? 0.f : row_lse * kLog2e, dl = feed.seg == kNoSeg ? 0.f : row_delta;
+                if (far) {
+                    float low = 0.f;
+                    if (feed.seg != kNoSeg && far_lse(row_lse)) {
+                        const float* const two = a.far + 2 * (((int64_t)batch * a.heads + kvh * a.group + h) * a.length + q0 + lane);
+                        less = two[0], low = two[1];
+                    }
+                    sh.low[lane] = low;
+                }
+                if (masked && (!(fabsf(less) < INFINITY) || !(fabsf(dl) < INFINITY))) {
+                    less = dl = 0.f;
                     atomicOr(&sh.bad[parity][lane >> 5], 1u << (lane & 31));
                 }
-                sh.lse[lane] = lse2;
+                sh.less[lane] = less;
                 sh.delta[lane] = dl;
                 if (lane < 2) sh.bad[parity ^ 1][lane] = 0u;          // last read before the barrier above
             }
             if (flat < 0 && tid < 2 * kTile - 1)
-                sh.bias[tid] = table[bucket_of(a.bk, sh.border, lo + tid)] * kLog2e;
+                sh.bias[tid] = table_log2(table[bucket_of(a.bk, sh.border, lo + tid)]);
         }
         round = after(SPLIT > 1 ? after(round) : round);
         at = set ? after(round) : round;
@@ -137,16 +148,19 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
         if (sees) {
             f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
             first_product<T, DP>(s, kf, rd, sh.q);
-            to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? table[flat] * kLog2e : 0.f);
+            to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? table_log2(table[flat]) : 0.f);
             if (flat < 0) add_bias(s, &sh.bias[4 * g - (k - k0) + kTile - 1]);
 #pragma unroll
-            for (int n = 0; n < 4; ++n) s[n] -= *reinterpret_cast<const f32x4*>(&sh.lse[16 * n + 4 * g]);
-            // rows are marked for the block: also where this wave's keys are visible to the whole tile
-            if (masked && (sh.bad[parity][0] | sh.bad[parity][1])) spoil_rows(s, sh.bad[parity], g);
-            if (!whole(t, wk0 + 15, mixed)) {
-                // rows past the history's end are no one's segment; without weight, whatever their bias is
-                if (mixed || q0 + kTile > a.length) mask_scores<true, true>(s, sh.seg, own, first - q0, lane);
-                else mask_scores<false, true>(s, sh.seg, own, first - q0, lane);
+            for (int n = 0; n < 4; ++n) s[n] -= *reinterpret_cast<const f32x4*>(&sh.less[16 * n + 4 * g]);
+            if (masked || far) {
+                if (far) {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) s[n] -= *reinterpret_cast<const f32x4*>(&sh.low[16 * n + 4 * g]);
+                }
+                // rows are marked for the block: also where this wave's keys are visible to the whole tile
+                if (sh.bad[parity][0] | sh.bad[parity][1]) spoil_rows(s, sh.bad[parity], g);
+                if (mixed) mask_scores<true, true>(s, sh.seg, own, first - q0, lane, a.length - first);
+                else mask_scores<false, true>(s, sh.seg, own, first - q0, lane, a.length - first);
             }
 #pragma unroll
             for (int n = 0; n < 4; ++n)

@@ -22,6 +22,7 @@ template <typename T, int DP> struct DqShared {
     float bias[2 * kTile];
     float table[kMaxBorders];
     int border[kMaxBorders];
+    float base[kTile];                             // of rows whose lse is far from zero
     float strip[kWavesPerBlock][4][kStrip];        // see table_near
     float bucket[kWavesPerBlock][kMaxBorders];     // sums of ds by bucket, each wave's own
     TileMarks marks;
@@ -75,7 +76,12 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
         delta = group_sum(delta);
     }
     const float lse = a.lse[stat];
-    const float lse2 = lse == -INFINITY ? 0.f : lse * kLog2e;     // a row that sees nothing: all its pairs are masked
+    // whether any row is far, of the wave or, where its waves have to agree, of the block
+    float any_lse = lse;
+    if (KEEP == 0) any_lse = a.lse[((int64_t)batch * a.heads + head) * a.length + (q0 + lane < a.length ? q0 + lane : a.length - 1)];
+    const bool far = __any(far_lse(any_lse));
+    if (KEEP == 0 && far && tid < kTile) sh.base[tid] = 0.f;
+    float less = lse == -INFINITY ? 0.f : lse * kLog2e;           // a row that sees nothing: all its pairs are masked
     const int own = live ? qseg : kNoSegOwner;
     const int ntiles = (a.length + kTile - 1) / kTile;
     int t1 = ntiles;
@@ -86,7 +92,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
         t1 = t1 < ntiles ? t1 : ntiles;
     }
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
-    if (tid < buckets) sh.table[tid] = a.table[(int64_t)head * buckets + tid] * kLog2e;
+    if (tid < buckets) sh.table[tid] = table_log2(a.table[(int64_t)head * buckets + tid]);
     if (tid < kMaxBorders) sh.border[tid] = kernel_borders()[tid];
     if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;
@@ -112,6 +118,8 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
         feed.load(kp + k0 * a.k.sr, a.k.sr, vp + k0 * a.v.sr, a.v.sr, k0, a.length, seg, a.dim);
     };
     const int tfirst = next_tile(0, t1, mk);
+    constexpr bool EARLY = KEEP > 2;                 // the next tile's loads on their way: 1.03 ms and 1.09; two tiles would lose a
+    bool loaded = false;                             // wave per SIMD to it (1024 x 100, heads of 64: 15 us and 14)
     const bool one_tile = TABLE && next_tile(tfirst + 1, t1, mk) >= t1;
 
     f32x4 dq[MEND ? 2 : 1][S::DT];                                // ds k, p k
@@ -137,21 +145,35 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
         return a.bk.side ? uniform_bucket(a.bk, hi - 2 * kTile + 2, hi) : 0;
     };
     auto sees = [&](int t) { return wq0 < a.length && !(a.causal && t * kTile > wq0 + 15 && t * kTile >= prefix); };
-    // weights and dp of a tile in LDS
-    auto weigh = [&](int t, bool mixed, f32x4 (&s)[4], f32x4 (&dp)[4], f32x4 (&slope)[CAP ? 4 : 1]) {
+    // scores of a tile in LDS
+    auto score = [&](int t, bool mixed, f32x4 (&s)[4], f32x4 (&slope)[CAP ? 4 : 1]) {
         const int k0 = t * kTile, flat = flat_of(t);
         first_product<T, DP>(s, qf, rd, sh.k);
         to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? sh.table[flat] : 0.f);
         if (flat < 0) add_bias(s, &sh.bias[4 * g - (q - q0) + kTile - 1]);
-        if (!whole(t, wq0, mixed) || !full_rows) {
+        if (!whole(t, wq0, mixed) || !full_rows || (KEEP == 0 && far)) {
+            if (KEEP == 0 && far) {                               // weights are 2^(s - base - less)
+                const float base = sh.base[wave * 16 + c];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) s[n] -= base;
+            }
             if (mixed) mask_scores<true, false>(s, sh.seg, own, last - k0, lane);
             else mask_scores<false, false>(s, sh.seg, own, last - k0, lane);
         }
+    };
+    // weights and dp of a tile in LDS
+    auto weigh = [&](int t, bool mixed, f32x4 (&s)[4], f32x4 (&dp)[4], f32x4 (&slope)[CAP ? 4 : 1]) {
+        score(t, mixed, s, slope);
         first_product<T, DP>(dp, df, rd, sh.v);
+        if (KEEP > 0 && far) {                                    // weights follow when all tiles have been seen
+#pragma unroll
+            for (int n = 0; n < 4; ++n) s[n] -= less;
+            return;
+        }
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - lse2);
+            for (int r = 0; r < 4; ++r) s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - less);
     };
     auto add_seen = [&](const f32x4 (&s)[4], const f32x4 (&dp)[4]) {
 #pragma unroll
@@ -187,7 +209,8 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
         constexpr bool DELTA = decltype(delta_only)::value;
         auto after = [&](int t) { return next_tile(t + 1, t1, mk); };
         int round = tfirst, t = set ? after(round) : round;       // the first set's tile and this one's
-        if (AHEAD && t < t1) load(t);
+        if (AHEAD && !loaded && t < t1) load(t);
+        loaded = false;
         while (round < t1) {
             const bool there = SPLIT == 1 || t < t1, mixed = there && tile_mixed(mk, t);
             if (!AHEAD && there) load(t);
@@ -232,12 +255,48 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
             }
         }
     };
+    auto load_first = [&] {
+        const int t = set ? next_tile(tfirst + 1, t1, mk) : tfirst;
+        if (AHEAD || EARLY) load(t < t1 ? t : 0), loaded = true;
+    };
+    load_first();
+    if (KEEP == 0 && far) {                          // a walk over the keys for the maximum and sum of rows that are far
+        float top = -INFINITY, sum = 0.f;
+        for (int t = tfirst; t < t1; t = next_tile(t + 1, t1, mk)) {
+            const bool mixed = tile_mixed(mk, t);
+            load(t);
+            __syncthreads();
+            feed.template put<false>(sh.k, sh.v, sh.seg, !whole(t, q0, mixed), nullptr);
+            put_bias(t);
+            __syncthreads();
+            if (!sees(t)) continue;
+            f32x4 s[4], slope[CAP ? 4 : 1];
+            score(t, mixed, s, slope);
+            float most = top;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) most = fmaxf(most, fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])));
+            most = group_max(most);
+            const float from = most == -INFINITY ? 0.f : most;
+            sum *= __builtin_amdgcn_exp2f(top - from);
+            top = most;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(s[n][r] - from);
+        }
+        sum = group_sum(sum);
+        if (live && far_lse(lse)) {
+            less = __builtin_amdgcn_logf(sum);
+            if (g == 0) sh.base[wave * 16 + c] = top;
+            if (g == 0 && set == 0) a.far[2 * stat] = top, a.far[2 * stat + 1] = less;
+        }
+        __syncthreads();
+        load_first();
+    }
     if constexpr (KEEP > 0) {
         f32x4 s[KEEP][4], dp[KEEP][4], none[1];
         int tile[KEEP];
         int t = tfirst;
-        constexpr bool EARLY = KEEP > 2;             // the next tile's loads on their way: 1.03 ms and 1.09; two tiles would
-        if (EARLY) load(t < t1 ? t : 0);             // lose a wave per SIMD to it (1024 x 100, heads of 64: 15 us and 14)
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
             tile[i] = t;
@@ -252,10 +311,42 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
                 __syncthreads();
                 if (sees(t)) {
                     weigh(t, mixed, s[i], dp[i], none);
-                    add_seen(s[i], dp[i]);
+                    if (!far) add_seen(s[i], dp[i]);
                 }
                 t = tn;
             }
+        }
+        if (far) {                                   // s are scores less the rounded lse: what is left of a row's maximum, and its sum
+            const bool mine = live && far_lse(lse);
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+                if (tile[i] < t1 && sees(tile[i]))
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) top = fmaxf(top, fmaxf(fmaxf(s[i][n][0], s[i][n][1]), fmaxf(s[i][n][2], s[i][n][3])));
+            top = group_max(top);
+            top = mine ? top : 0.f;
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+                if (tile[i] < t1 && sees(tile[i]))
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        s[i][n] -= top;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(s[i][n][r]);
+                    }
+            sum = group_sum(sum);
+            const float low = mine ? __builtin_amdgcn_logf(sum) : 0.f;
+            if (mine && g == 0) a.far[2 * stat] = less + top, a.far[2 * stat + 1] = low;
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+                if (tile[i] < t1 && sees(tile[i])) {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[i][n][r] = __builtin_amdgcn_exp2f(s[i][n][r] - low);
+                    add_seen(s[i], dp[i]);
+                }
         }
         delta = group_sum(seen);
         auto load_keys = [&](int n) {

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend(const AttArgs 
         t1 = t1 < ntiles ? t1 : ntiles;
     }
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
-    if (tid < buckets) sh.table[tid] = a.table[(int64_t)head * buckets + tid] * kLog2e;
+    if (tid < buckets) sh.table[tid] = table_log2(a.table[(int64_t)head * buckets + tid]);
     if (tid < kMaxBorders) sh.border[tid] = kernel_borders()[tid];
     if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;

@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
     for (int h = 0; h < a.group; ++h) {
         const int head = kvh * a.group + h;
         const float lse = lse_ahead;
-        if (tid < buckets) sh.table[tid] = a.table[(int64_t)head * buckets + tid] * kLog2e;
+        if (tid < buckets) sh.table[tid] = table_log2(a.table[(int64_t)head * buckets + tid]);
         __syncthreads();                                        // the last head's tiles have been read; table and bad are set
         queries.template put<false>(sh.q, sh.d, sh.seg, masked, sh.bad);
         if (flat < 0 && tid < 2 * kTile - 1) sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, kTile - 1 - tid)];
@@ -141,8 +141,9 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
         }
         __syncthreads();
         // a query that holds a non-finite value, or sees one, has NaN for its statistics: the pairs that it sees are NaN
-        float lse2 = lse == -INFINITY ? 0.f : lse * kLog2e;
-        if ((sh.bad[w0 >> 5] >> (row & 31)) & 1) lse2 = NAN;
+        float less = lse == -INFINITY ? 0.f : lse * kLog2e;
+        const bool spoilt = (sh.bad[w0 >> 5] >> (row & 31)) & 1;
+        if (spoilt) less = NAN;
         f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
         {
             u32x4 f[S::KK];
@@ -156,8 +157,25 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
         to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? sh.table[flat] : 0.f);
         if (flat < 0) add_bias(s, &sh.bias[4 * g - row + kTile - 1]);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) s[n] -= lse2;
+        for (int n = 0; n < 4; ++n) s[n] -= less;
         if (masked) mask_scores<true, false>(s, sh.seg, own, last, lane);
+        const bool far = own >= 0 && far_lse(lse);
+        if (__any(far)) {                                       // what is left of their maximum, and their sum
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) top = fmaxf(top, fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])));
+            top = group_max(top);
+            top = far && !spoilt ? top : 0.f;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                s[n] -= top;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(s[n][r]);
+            }
+            const float low = __builtin_amdgcn_logf(group_sum(sum));
+#pragma unroll
+            for (int n = 0; n < 4; ++n) s[n] -= far && !spoilt ? low : 0.f;
+        }
         float delta = 0.f;
 #pragma unroll
         for (int n = 0; n < 4; ++n)

@@ -143,3 +143,69 @@ def test_a_step_whose_scores_are_all_minus_infinity_yields_zeros(dtype):
             work = torch.empty(plan.step_bytes(4, rows), dtype=torch.uint8, device="cuda")
             plan.step(q.cuda(), kn.cuda(), vn.cuda(), kc.cuda(), vc.cuda(), lens.cuda(), O, work, table=table.cuda())
             lo.assert_within(O, (o, bound), f"o of {rows}, {hidden} hidden")
+
+
+def gradients(torch, gram, c, q, k, v, do, seg, prefix, table, table_gradient):
+    """As run_gpu, with or without the table's gradient."""
+    plan = plan_of(gram, c)
+    B, L, H = c["B"], c["L"], c["H"]
+    Q, K, V, DO = (placed(torch, t, c["layout"]) for t in (q, k, v, do))
+    O, DQ, DK, DV = (placed(torch, torch.full_like(t, float("nan")), c["layout"]) for t in (q, q, k, v))
+    seg, prefix, table = (None if t is None else t.cuda() for t in (seg, prefix, table))
+    lse = torch.full((B, H, L), float("nan"), device="cuda")
+    plan.forward(Q, K, V, O, lse=lse, segments=seg, prefix=prefix, table=table)
+    work = torch.full((plan.backward_bytes(B, L),), 255, dtype=torch.uint8, device="cuda")      # NaN wherever it is read as floats
+    dtable = torch.full((H, c["buckets"]), float("nan"), device="cuda") if table_gradient else None
+    plan.backward(Q, K, V, O, lse, DO, DQ, DK, DV, work, segments=seg, prefix=prefix, table=table, dtable=dtable)
+    out = dict(o=O, lse=lse, dq=DQ, dk=DK, dv=DV)
+    return {**out, "dtable": dtable} if table_gradient else out
+
+
+FAR = [
+    case("f32", 2, 70, 2, 1, 16, buckets=8, far=40), case("bf16", 1, 200, 2, 2, 64, pad="holes", buckets=16, far=64),
+    case("bf16", 66, 70, 2, 2, 20, buckets=8, far=40), case("f32", 3, 40, 4, 2, 24, docs=True, buckets=8, far=40),
+    case("bf16", 3, 50, 2, 2, 20, pad="tail", prefix=True, buckets=8, far=40, both=True), case("f32", 1, 150, 2, 2, 128, causal=False, buckets=8, far=40, both=True),
+    case("bf16", 33, 260, 4, 2, 36, cap=5.0, buckets=8, far=40), case("bf16", 1, 300, 2, 1, 128, docs=True, prefix=True, buckets=32, far=128, both=True),
+    case("bf16", 50, 200, 2, 2, 128, docs=True, buckets=8, far=40), case("f32", 1, 64, 2, 2, 64, cap=5.0, buckets=1, far=2),
+    case("f32", 1, 129, 1, 1, 127, layout="odd", buckets=8, far=40),
+]
+
+
+@pytest.mark.parametrize("table_gradient", [True, False])
+@pytest.mark.parametrize("bias", [300.0, -70000.0, -1e9])
+@pytest.mark.parametrize("c", FAR, ids=name_of)
+def test_a_bias_that_all_pairs_share_changes_no_weight(c, bias, table_gradient):
+    """However far from zero it is, where the sum of a row's weights is lost beside it.  The products are too small to count
+    (q is 2^-60 of what it would be), so all weights of a row are the same."""
+    import torch
+    from paper_2204_04179_amd import gram
+    q, k, v, do, seg, prefix, table = inputs(torch, c, seed=41)
+    q = q * 2.0 ** -60
+    want = oracle_of(c, q, k, v, do, seg, prefix, torch.zeros_like(table) if table_gradient else None)
+    got = gradients(torch, gram, c, q, k, v, do, seg, prefix, torch.full_like(table, bias), table_gradient)
+    for n in got:
+        if n == "lse":
+            value, bound = want[n]
+            lo.assert_within(got[n], (value + bias, bound + 8 * lo.U * abs(bias)), n)
+        else:
+            lo.assert_within(got[n], want[n], n)
+
+
+@pytest.mark.parametrize("table_gradient", [True, False])
+@pytest.mark.parametrize("bias", [-1e9, -1.23e7, -3.3e10])
+@pytest.mark.parametrize("c", FAR, ids=name_of)
+def test_a_bias_that_hides_each_position_from_itself(c, bias, table_gradient):
+    """At distance 0, as programs mask: the first position of a session sees nothing else and has weight one."""
+    import torch
+    from paper_2204_04179_amd import gram
+    *data, table = inputs(torch, c, seed=42)
+    mild = table.clone()
+    table[:, 0], mild[:, 0] = bias, -100.0             # exp(-90) is nothing beside the others
+    if c["buckets"] == 1:
+        mild[:] = 0.0
+        data[0] = data[0] * 2.0 ** -60
+    want = oracle_of(c, *data, mild)
+    got = gradients(torch, gram, c, *data, table, table_gradient)
+    for n in got:
+        if n != "lse":
+            lo.assert_within(got[n], want[n], n)
