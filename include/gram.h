@@ -425,7 +425,10 @@ int gram_layer_norm_backward(const void* x, int32_t x_dtype, const float* weight
  *   s = c + table[h, bucket(i - j)]          (no bias if buckets is 0)
  *   o_i = sum_j softmax_j(s_ij) v_j          over the visible j
  * j is visible to i if segments[i] == segments[j] >= 0 and, with causal set,
- * j <= i or j < prefix.  A query that sees nothing yields a zero row.
+ * j <= i or j < prefix.  A query that sees nothing, or only scores of minus
+ * infinity, yields a zero row.  Finite entries of the table beyond +-2e38 all count
+ * as the end of their type: they hide a pair from queries that see others, and a
+ * query that sees nothing else has the mean of the values (and that end as its lse).
  *
  * Buckets of a distance n = i - j, S of them to a side: n < S/2 (rounded down, e)
  * has bucket n; a larger n has the largest b < S with

@@ -375,11 +375,21 @@ __device__ __forceinline__ float tanh_f32(float x)
     return fabsf(x) < 0.4f ? s : far;
 }
 
-// An entry of the table in units of log 2, rounded by itself wherever it is used, so that a pair has the same score in every pass.
-__device__ __forceinline__ float table_log2(float entry)
+// A bias or lse in units of log 2, rounded by itself wherever it is used, so that a pair has the same score in every pass.  Finite ones
+// stay finite, with room for a product beside them: the lowest number of the type hides a pair from rows that see others, and
+// no more than that.
+constexpr float kMostScore = 3e38f;
+__device__ __forceinline__ float to_log2(float x)
 {
 #pragma clang fp contract(off)
-    return entry * kLog2e;
+    const float y = x * kLog2e;
+    return fabsf(x) < INFINITY ? __builtin_amdgcn_fmed3f(y, -kMostScore, kMostScore) : y;
+}
+// And back: the log of a row's sum.  At the end of the range it is the end of the type.
+__device__ __forceinline__ float row_lse(float top, float total)
+{
+    const float lse = top * kLn2 + logf(total);
+    return fabsf(top) >= kMostScore && fabsf(lse) < INFINITY ? copysignf(3.402823466e38f, top) : lse;
 }
 
 // A tile's products to scores in units of log 2: scaled, capped, with the bias `flat2` of the whole tile; slope (capped

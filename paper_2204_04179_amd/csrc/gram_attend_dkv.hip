@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
             far = __any(feed.seg != kNoSeg && far_lse(row_lse));
             if (wave == 0) {
                 // a query whose statistics are not finite sees a non-finite value; it is marked like one that holds it
-                float less = row_lse == -INFINITY || feed.seg == kNoSeg ? 0.f : row_lse * kLog2e, dl = feed.seg == kNoSeg ? 0.f : row_delta;
+                float less = row_lse == -INFINITY || feed.seg == kNoSeg ? 0.f : to_log2(row_lse), dl = feed.seg == kNoSeg ? 0.f : row_delta;
                 if (far) {
                     float low = 0.f;
                     if (feed.seg != kNoSeg && far_lse(row_lse)) {
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
                 if (lane < 2) sh.bad[parity ^ 1][lane] = 0u;          // last read before the barrier above
             }
             if (flat < 0 && tid < 2 * kTile - 1)
-                sh.bias[tid] = table_log2(table[bucket_of(a.bk, sh.border, lo + tid)]);
+                sh.bias[tid] = to_log2(table[bucket_of(a.bk, sh.border, lo + tid)]);
         }
         round = after(SPLIT > 1 ? after(round) : round);
         at = set ? after(round) : round;
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
         if (sees) {
             f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
             first_product<T, DP>(s, kf, rd, sh.q);
-            to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? table_log2(table[flat]) : 0.f);
+            to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? to_log2(table[flat]) : 0.f);
             if (flat < 0) add_bias(s, &sh.bias[4 * g - (k - k0) + kTile - 1]);
 #pragma unroll
             for (int n = 0; n < 4; ++n) s[n] -= *reinterpret_cast<const f32x4*>(&sh.less[16 * n + 4 * g]);

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
     if (KEEP == 0) any_lse = a.lse[((int64_t)batch * a.heads + head) * a.length + (q0 + lane < a.length ? q0 + lane : a.length - 1)];
     const bool far = __any(far_lse(any_lse));
     if (KEEP == 0 && far && tid < kTile) sh.base[tid] = 0.f;
-    float less = lse == -INFINITY ? 0.f : lse * kLog2e;           // a row that sees nothing: all its pairs are masked
+    float less = lse == -INFINITY ? 0.f : to_log2(lse);           // a row that sees nothing: all its pairs are masked
     const int own = live ? qseg : kNoSegOwner;
     const int ntiles = (a.length + kTile - 1) / kTile;
     int t1 = ntiles;
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
         t1 = t1 < ntiles ? t1 : ntiles;
     }
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
-    if (tid < buckets) sh.table[tid] = table_log2(a.table[(int64_t)head * buckets + tid]);
+    if (tid < buckets) sh.table[tid] = to_log2(a.table[(int64_t)head * buckets + tid]);
     if (tid < kMaxBorders) sh.border[tid] = kernel_borders()[tid];
     if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend(const AttArgs 
         t1 = t1 < ntiles ? t1 : ntiles;
     }
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
-    if (tid < buckets) sh.table[tid] = table_log2(a.table[(int64_t)head * buckets + tid]);
+    if (tid < buckets) sh.table[tid] = to_log2(a.table[(int64_t)head * buckets + tid]);
     if (tid < kMaxBorders) sh.border[tid] = kernel_borders()[tid];
     if (seg) mark_tiles(sh.marks, seg, a.length, qseg, q < a.length, 0, t1);
     const TileMarks* const mk = seg ? &sh.marks : nullptr;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend(const AttArgs 
         T* const op = static_cast<T*>(a.o.data) + batch * a.o.sb + head * a.o.sh + wq0 * a.o.sr;
         store_rows<T, DP, UNIT>(sh.k + wave * 16 * S::RB, o, empty ? 0.f : 1.f / total, op, a.o.sr, a.length - wq0, a.dim, lane);
         if (a.lse && g == 0 && q < a.length)
-            a.lse[((int64_t)batch * a.heads + head) * a.length + q] = empty ? -INFINITY : top * kLn2 + logf(total);
+            a.lse[((int64_t)batch * a.heads + head) * a.length + q] = empty ? -INFINITY : row_lse(top, total);
     }
 }
 

@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
     for (int h = 0; h < a.group; ++h) {
         const int head = kvh * a.group + h;
         const float lse = lse_ahead;
-        if (tid < buckets) sh.table[tid] = table_log2(a.table[(int64_t)head * buckets + tid]);
+        if (tid < buckets) sh.table[tid] = to_log2(a.table[(int64_t)head * buckets + tid]);
         __syncthreads();                                        // the last head's tiles have been read; table and bad are set
         queries.template put<false>(sh.q, sh.d, sh.seg, masked, sh.bad);
         if (flat < 0 && tid < 2 * kTile - 1) sh.bias[tid] = sh.table[bucket_of(a.bk, sh.border, kTile - 1 - tid)];
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
         }
         __syncthreads();
         // a query that holds a non-finite value, or sees one, has NaN for its statistics: the pairs that it sees are NaN
-        float less = lse == -INFINITY ? 0.f : lse * kLog2e;
+        float less = lse == -INFINITY ? 0.f : to_log2(lse);
         const bool spoilt = (sh.bad[w0 >> 5] >> (row & 31)) & 1;
         if (spoilt) less = NAN;
         f32x4 s[4], dp[4], slope[CAP ? 4 : 1];

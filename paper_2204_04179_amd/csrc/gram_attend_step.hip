@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB <= 128 ? 3 : 2)) void k_s
 
     const int buckets = a.bk.two_sided ? 2 * a.bk.side : a.bk.side;
     for (int i = threadIdx.x; i < heads_here * buckets; i += kBlock)
-        s_table[i / buckets][i % buckets] = table_log2(a.table[(int64_t)head0 * buckets + i]);
+        s_table[i / buckets][i % buckets] = to_log2(a.table[(int64_t)head0 * buckets + i]);
     if (threadIdx.x < kMaxBorders) s_border[threadIdx.x] = a.bk.border[threadIdx.x];
 
     u32x4 qf[S::KK];

@@ -209,3 +209,43 @@ def test_a_bias_that_hides_each_position_from_itself(c, bias, table_gradient):
     for n in got:
         if n != "lse":
             lo.assert_within(got[n], want[n], n)
+
+
+@pytest.mark.parametrize("table_gradient", [True, False])
+@pytest.mark.parametrize("bias", ["lowest", "highest", -2.5e38])
+@pytest.mark.parametrize("c", FAR, ids=name_of)
+def test_a_bias_at_the_end_of_its_type(c, bias, table_gradient):
+    """The lowest finite number is no minus infinity: where all that a row sees has it, the row is the mean of its values."""
+    import torch
+    from paper_2204_04179_amd import gram
+    big = torch.finfo(torch.float32).max
+    entry = {"lowest": -big, "highest": big}.get(bias, bias)
+    q, k, v, do, seg, prefix, table = inputs(torch, c, seed=43)
+    q = q * 2.0 ** -60
+    want = oracle_of(c, q, k, v, do, seg, prefix, torch.zeros_like(table) if table_gradient else None)
+    got = gradients(torch, gram, c, q, k, v, do, seg, prefix, torch.full_like(table, entry), table_gradient)
+    for n in got:
+        if n != "lse":
+            lo.assert_within(got[n], want[n], n)
+    lse = got["lse"].cpu()
+    nothing = torch.isinf(want["lse"][0])
+    assert bool((lse[~nothing] == (big if entry > 0 else -big)).all()) and bool((lse[nothing] == -float("inf")).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [40, 1500])
+def test_a_step_with_a_bias_at_the_end_of_its_type(dtype, rows):
+    import torch
+    from paper_2204_04179_amd import gram
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    lens = torch.tensor([0, rows - 1, rows // 2], dtype=torch.int32)
+    q, kn, vn = draw(torch, (3, 4, 16), 1, dt) * 2.0 ** -60, draw(torch, (3, 2, 16), 2, dt), draw(torch, (3, 2, 16), 3, dt)
+    kc, vc = draw(torch, (3, rows, 2, 16), 4, dt), draw(torch, (3, rows, 2, 16), 5, dt)
+    plan = gram.HistoryAttention(4, 2, 16, dtype=gram.F32 if dtype == "f32" else gram.BF16, buckets=8, max_distance=20)
+    o, bound, _, _ = lo.step(q, kn, vn, kc, vc, lens, scale=0.25, table=torch.zeros(4, 8), far=20)
+    for sign in (-1.0, 1.0):
+        table = torch.full((4, 8), sign * torch.finfo(torch.float32).max)
+        O = torch.full((3, 4, 16), float("nan"), dtype=dt, device="cuda")
+        work = torch.empty(plan.step_bytes(3, rows), dtype=torch.uint8, device="cuda")
+        plan.step(q.cuda(), kn.cuda(), vn.cuda(), kc.cuda(), vc.cuda(), lens.cuda(), O, work, table=table.cuda())
+        lo.assert_within(O, (o, bound), "o")
