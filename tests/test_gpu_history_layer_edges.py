@@ -249,3 +249,15 @@ def test_a_step_with_a_bias_at_the_end_of_its_type(dtype, rows):
         work = torch.empty(plan.step_bytes(3, rows), dtype=torch.uint8, device="cuda")
         plan.step(q.cuda(), kn.cuda(), vn.cuda(), kc.cuda(), vc.cuda(), lens.cuda(), O, work, table=table.cuda())
         lo.assert_within(O, (o, bound), "o")
+
+
+# ---- many heads on one key head ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,rows,H,KV,D,cap,buckets,far,first,layout", [
+    (3, 70, 17, 1, 64, 0.0, 8, 20, False, "rows"), (2, 1500, 40, 1, 36, 30.0, 32, 128, True, "odd"), (4, 600, 34, 2, 128, 0.0, 16, 64, False, "heads"),
+    (2, 33, 32, 1, 20, 4.0, 0, 0, False, "rows"), (3, 1030, 50, 2, 128, 0.0, 64, 300, False, "rows")])
+def test_a_step_of_more_heads_than_a_block_takes(dtype, B, rows, H, KV, D, cap, buckets, far, first, layout):
+    """Sixteen query heads of a key head go to one block, the next sixteen to another."""
+    base.test_cached_step(dtype, B, rows, H, KV, D, cap, buckets, far, False, first, layout)
