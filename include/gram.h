@@ -547,7 +547,8 @@ int gram_profile_enable(gram_ctx* ctx, uint64_t mask, int32_t max_launches);
 int gram_profile_read(gram_ctx* ctx, int k, int64_t* launches, double* total_ms);
 
 /* Message of the last failing call on ctx (or, when ctx is NULL, of the calling
- * thread's last failing gram_create or call without a context).  The string is owned by the library. */
+ * thread's last failing gram_create or call without a context; a thread that has
+ * none reads the last of all threads').  The string is owned by the library. */
 const char* gram_last_error(const gram_ctx* ctx);
 
 #ifdef __cplusplus

@@ -13,8 +13,26 @@ using namespace gram;
 
 namespace {
 
-// Message of the last failing call without a context; each thread has its own, since such calls may run side by side.
-thread_local char g_call_error[512] = "";
+// Message of the last failing call without a context; each thread has its own, since such calls may run side by side.  A thread
+// without one is told the last of all threads'.
+thread_local char g_call_error[512] = "", g_others_copy[512] = "";
+std::mutex g_any_mutex;
+char g_any_error[512] = "";
+
+void keep_call_error(const char (&message)[512])
+{
+    memcpy(g_call_error, message, sizeof g_call_error);
+    std::lock_guard<std::mutex> lock(g_any_mutex);
+    memcpy(g_any_error, message, sizeof g_any_error);
+}
+
+const char* call_error()
+{
+    if (g_call_error[0]) return g_call_error;
+    std::lock_guard<std::mutex> lock(g_any_mutex);
+    memcpy(g_others_copy, g_any_error, sizeof g_others_copy);
+    return g_others_copy;
+}
 
 int fail(Ctx* c, int code, const char* fmt, ...)
 {
@@ -23,7 +41,7 @@ int fail(Ctx* c, int code, const char* fmt, ...)
     va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    if (c) c->last_error = buf; else memcpy(g_call_error, buf, sizeof buf);
+    if (c) c->last_error = buf; else keep_call_error(buf);
     return code;
 }
 
@@ -262,10 +280,12 @@ namespace gram {
 
 int fail_call(int code, const char* fmt, ...)
 {
+    char buf[512];
     va_list ap;
     va_start(ap, fmt);
-    vsnprintf(g_call_error, sizeof g_call_error, fmt, ap);
+    vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
+    keep_call_error(buf);
     return code;
 }
 
@@ -811,7 +831,7 @@ int gram_check(gram_ctx* ctx, void* stream)
 const char* gram_last_error(const gram_ctx* ctx)
 {
     const Ctx* c = reinterpret_cast<const Ctx*>(ctx);
-    return c ? c->last_error.c_str() : g_call_error;
+    return c ? c->last_error.c_str() : call_error();
 }
 
 }  // extern "C"
