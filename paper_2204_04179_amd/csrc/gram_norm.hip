@@ -29,7 +29,7 @@ struct bf16_t { uint16_t bits; };
 template <typename T, int VEC> struct Raw {
     static constexpr int WORDS = VEC * (int)sizeof(T) / 4 > 0 ? VEC * (int)sizeof(T) / 4 : 1;
     uint32_t w[WORDS];
-    __device__ __forceinline__ void load(const T* __restrict__ p)
+    __device__ __forceinline__ void load(const T* p)
     {
         if constexpr (VEC == 1) {
             if constexpr (sizeof(T) == 2) w[0] = p->bits;
@@ -57,7 +57,7 @@ template <typename T, int VEC> struct Raw {
         else return __builtin_bit_cast(float, w[e]);
     }
 };
-template <int VEC, typename T> __device__ __forceinline__ void load_vec(const T* __restrict__ p, float* v)
+template <int VEC, typename T> __device__ __forceinline__ void load_vec(const T* p, float* v)
 {
     Raw<T, VEC> r;
     r.load(p);
@@ -65,7 +65,7 @@ template <int VEC, typename T> __device__ __forceinline__ void load_vec(const T*
     for (int e = 0; e < VEC; ++e) v[e] = r.get(e);
 }
 
-template <int VEC> __device__ __forceinline__ void store_vec(float* __restrict__ p, const float* v)
+template <int VEC> __device__ __forceinline__ void store_vec(float* p, const float* v)
 {
     if constexpr (VEC == 1) {
         *p = v[0];
@@ -78,7 +78,7 @@ template <int VEC> __device__ __forceinline__ void store_vec(float* __restrict__
     }
 }
 
-template <int VEC> __device__ __forceinline__ void store_vec(bf16_t* __restrict__ p, const float* v)
+template <int VEC> __device__ __forceinline__ void store_vec(bf16_t* p, const float* v)
 {
     if constexpr (VEC == 1) {
         p->bits = (uint16_t)pack_bf16x2(v[0], 0.f);
@@ -123,11 +123,11 @@ template <int LPR, int N> __device__ __forceinline__ void row_sum(float (&v)[N],
     }
 }
 
-// One row per group of LPR lanes, VEC neighbouring columns per lane and chunk, CPL chunks.
+// One row per group of LPR lanes, VEC neighbouring columns per lane and chunk, CPL chunks.  x and y may be the same rows.
 template <typename TX, typename TY, int VEC, int CPL, int LPR>
-__global__ __launch_bounds__(kBlock) void k_layer_norm(const TX* __restrict__ x, const float* __restrict__ w,
+__global__ __launch_bounds__(kBlock) void k_layer_norm(const TX* x, const float* __restrict__ w,
                                                        const float* __restrict__ b, const int* __restrict__ seg, int64_t m,
-                                                       int d, float inv_d, float eps, TY* __restrict__ y, float* __restrict__ stats)
+                                                       int d, float inv_d, float eps, TY* y, float* __restrict__ stats)
 {
     __shared__ float s_red[kWavesPerBlock];
     constexpr int RPB = kBlock / LPR;
