@@ -219,6 +219,23 @@ def _refuse(message):
     raise GramError(ERR_ARG, message)
 
 
+_INT_MAX = (1 << 31) - 1
+
+
+def _int(v, what):
+    """v as the library's 32-bit integers hold it: ctypes would wrap what does not fit."""
+    v = int(v)
+    if not -_INT_MAX <= v <= _INT_MAX:
+        _refuse(f"{what}: {v} does not fit 32 bits")
+    return v
+
+
+def _size(v):
+    """A size in a question about work buffers, -1 (which has none) where 32 bits do not hold it."""
+    v = int(v)
+    return v if v <= _INT_MAX else -1
+
+
 def _device():
     """The current device's index, and -1 where there is none (host tensors are then refused like any other's)."""
     import torch
@@ -254,7 +271,7 @@ def _work(t, what, size, dev):
 
 
 def layer_norm_work_bytes(m, d):
-    return int(load().gram_layer_norm_work_bytes(int(m), int(d)))
+    return int(load().gram_layer_norm_work_bytes(int(m), _size(d)))
 
 
 def _norm_rows(x, y, what, dev):
@@ -263,6 +280,8 @@ def _norm_rows(x, y, what, dev):
     if not x.is_cuda or x.get_device() != dev or not y.is_cuda or y.get_device() != dev:
         _refuse(f"{what}: not on the current device")
     d = x.shape[-1]
+    if d > _INT_MAX:
+        _refuse(f"{what}: a width that fits 32 bits expected, got {d}")
     return (x.numel() // d if d else 0), d
 
 
@@ -306,17 +325,18 @@ class HistoryAttention:
                  two_sided=False):
         import torch
         self._lib = load()
-        self.heads, self.kv_heads, self.head_dim, self.buckets = int(heads), int(kv_heads), int(head_dim), int(buckets)
+        what = "gram_attention: settings"
+        self.heads, self.kv_heads, self.head_dim, self.buckets = (_int(v, what) for v in (heads, kv_heads, head_dim, buckets))
         self.dtype = torch.bfloat16 if dtype == BF16 else torch.float32
-        self.cfg = GramAttentionConfig(self.heads, self.kv_heads, self.head_dim, int(dtype),
+        self.cfg = GramAttentionConfig(self.heads, self.kv_heads, self.head_dim, _int(dtype, what),
                                        max(float(head_dim), 1.0) ** -0.5 if scale is None else float(scale), float(cap),
-                                       1 if causal else 0, self.buckets, int(max_distance), 1 if two_sided else 0)
+                                       1 if causal else 0, self.buckets, _int(max_distance, what), 1 if two_sided else 0)
         self._cfg = C.byref(self.cfg)
         _ck_call(self._lib.gram_attention(self._cfg, 0, 0, None, None, None, None, None, None, None, None, None))
 
     def bucket(self, distance):
         """The bucket of the distance query position minus key position (-1 without a bias)."""
-        return int(self._lib.gram_distance_bucket(self._cfg, int(distance)))
+        return int(self._lib.gram_distance_bucket(self._cfg, max(-_INT_MAX, min(_INT_MAX, int(distance)))))
 
     def _operands(self, call, dev, *named):
         """gram_rows of the (name, tensor, shape) given, one after another; shapes of three dimensions have no rows."""
@@ -345,6 +365,8 @@ class HistoryAttention:
         if q.dim() != 4:
             _refuse("forward: q: [batch, length, heads, head_dim] expected")
         B, L, dev = q.shape[0], q.shape[1], _device()
+        if B > _INT_MAX or L > _INT_MAX:
+            _refuse("forward: batch and length that fit 32 bits expected")
         wide, shared = (B, L, self.heads, self.head_dim), (B, L, self.kv_heads, self.head_dim)
         rows = self._operands("forward", dev, ("q", q, wide), ("k", k, shared), ("v", v, shared), ("o", o, wide))
         at = rows.buffer_info()[0]
@@ -354,7 +376,7 @@ class HistoryAttention:
             _flat(lse, "forward: lse", torch.float32, B * self.heads * L, dev), _stream(stream)))
 
     def backward_bytes(self, batch, length):
-        return int(self._lib.gram_attention_backward_bytes(self._cfg, int(batch), int(length)))
+        return int(self._lib.gram_attention_backward_bytes(self._cfg, _size(batch), _size(length)))
 
     def backward(self, q, k, v, o, lse, do, dq, dk, dv, work, segments=None, prefix=None, table=None, dtable=None,
                  stream=None):
@@ -366,6 +388,8 @@ class HistoryAttention:
         if dtable is not None and self.buckets == 0:
             _refuse("backward: dtable without buckets")
         B, L, dev, H, i32, f32 = q.shape[0], q.shape[1], _device(), self.heads, torch.int32, torch.float32
+        if B > _INT_MAX or L > _INT_MAX:
+            _refuse("backward: batch and length that fit 32 bits expected")
         wide, shared = (B, L, H, self.head_dim), (B, L, self.kv_heads, self.head_dim)
         rows = self._operands("backward", dev, ("q", q, wide), ("k", k, shared), ("v", v, shared), ("o", o, wide),
                               ("do", do, wide), ("dq", dq, wide), ("dk", dk, shared), ("dv", dv, shared))
@@ -378,7 +402,7 @@ class HistoryAttention:
             _work(work, "backward: work", self._lib.gram_attention_backward_bytes(self._cfg, B, L), dev), _stream(stream)))
 
     def step_bytes(self, batch, capacity):
-        return int(self._lib.gram_attention_step_bytes(self._cfg, int(batch), int(capacity)))
+        return int(self._lib.gram_attention_step_bytes(self._cfg, _size(batch), _size(capacity)))
 
     def step(self, q, k_new, v_new, k_cache, v_cache, lengths, o, work, first=None, table=None, stream=None):
         """One new item per history: k_new, v_new ([batch, kv_heads, head_dim]) are written to row lengths[b] of the
@@ -388,6 +412,8 @@ class HistoryAttention:
         if q.dim() != 3 or k_cache.dim() != 4:
             _refuse("step: q [batch, heads, head_dim] and caches [batch, capacity, kv_heads, head_dim] expected")
         B, rows_max, dev, KV, D = q.shape[0], k_cache.shape[1], _device(), self.kv_heads, self.head_dim
+        if B > _INT_MAX or rows_max > _INT_MAX:
+            _refuse("step: batch and capacity that fit 32 bits expected")
         wide, new, cache = (B, self.heads, D), (B, KV, D), (B, rows_max, KV, D)
         rows = self._operands("step", dev, ("q", q, wide), ("k_new", k_new, new), ("v_new", v_new, new),
                               ("k_cache", k_cache, cache), ("v_cache", v_cache, cache), ("o", o, wide))
