@@ -253,10 +253,15 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
 
 bool attend_backward_short(const gram_attention_config& c, AttArgs a, int unit, hipStream_t s)
 {
-    // four tiles of rows and two of weights have to fit a CU's LDS: float32 rows of more than 64 elements do not.  Against a launch
-    // for the queries and one for the keys: 64 x 50, 4 heads of 128, 17 us and 22; 1024 x 60, 4 heads of 64 in float32, 205 and 221;
-    // 1024 x 50, 4 heads of 128, 142 and 145, but with the table's gradient 180 and 164.
+    // Four tiles of rows and two of weights have to fit a CU's LDS: float32 rows of more than 64 elements do not.  Against a launch
+    // for the queries and one for the keys: 64 x 50, 4 heads of 128, 12 us and 17, with the table's gradient 17 and 21; 1024 x 60, 4
+    // heads of 64 in float32, 205 and 221.
     if (a.length > kTile || (c.dtype == GRAM_F32 && c.head_dim > 64)) return false;
+    // Rows of 256 bytes leave room for one block per CU, which a second one waits for: beyond that many blocks short histories, whose
+    // tile is mostly empty, are faster in two launches, and so are most with the table's gradient, which the waves work out in
+    // turn with their barriers.  1024 histories, 4 heads of 128, one launch and two, with that gradient and without: 20
+    // positions 164 us and 123, 129 and 103; 50 positions 180 and 161, 145 and 148; 64 positions, 2 key heads for 8, 252 and 266 with it.
+    if (c.head_dim > 64 && a.batch * a.kv_heads > kFewBlocks && (a.length <= 32 || (a.part && a.length <= 56))) return false;
     a.items = a.batch * a.kv_heads;
     a.by_heads = FastDiv::of(a.kv_heads);
     by_shape_and_cap(c, unit, [&](auto type, auto dp, auto u, auto cap) {

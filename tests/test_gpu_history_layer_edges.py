@@ -261,3 +261,23 @@ def test_a_step_with_a_bias_at_the_end_of_its_type(dtype, rows):
 def test_a_step_of_more_heads_than_a_block_takes(dtype, B, rows, H, KV, D, cap, buckets, far, first, layout):
     """Sixteen query heads of a key head go to one block, the next sixteen to another."""
     base.test_cached_step(dtype, B, rows, H, KV, D, cap, buckets, far, False, first, layout)
+
+
+# ---- more histories of one tile than there are CUs, heads of more than 64 -----------------------------------
+
+ONE_TILE = [
+    case("bf16", 70, 20, 4, 4, 100, pad="tail", buckets=8, far=12), case("bf16", 90, 32, 3, 3, 128, docs=True), case("bf16", 130, 50, 4, 2, 72, prefix=True, buckets=32, far=40, both=True),
+    case("bf16", 130, 50, 4, 2, 128, pad="holes", cap=5.0), case("bf16", 66, 60, 4, 4, 128, buckets=8, far=12), case("bf16", 300, 1, 1, 1, 65, buckets=2, far=3),
+]
+
+
+@pytest.mark.parametrize("c", ONE_TILE, ids=name_of)
+def test_many_histories_of_one_tile_and_wide_heads(c):
+    base.test_attention_and_its_backward(c)
+
+
+@pytest.mark.parametrize("c", [ONE_TILE[0], ONE_TILE[4]], ids=name_of)
+def test_biases_far_from_zero_among_many_histories_of_one_tile(c):
+    for table_gradient in (True, False):
+        test_a_bias_that_all_pairs_share_changes_no_weight(c, -1e9, table_gradient)
+        test_a_bias_at_the_end_of_its_type(c, "lowest", table_gradient)
