@@ -311,6 +311,11 @@ template <typename T> __device__ __forceinline__ float dot_chunk(u32x4 x, u32x4 
     return sum;
 }
 
+// Product with a weight: zero where either is, whatever the other.  A masked pair has weight zero, and the product beside it may have
+// overflowed although all values are finite.
+__device__ float mul_zero(float, float) __asm("llvm.amdgcn.fmul.legacy");       // v_mul_legacy_f32
+__device__ __forceinline__ float weighed(float weight, float x) { return mul_zero(weight, x); }
+
 // ---- lanes ------------------------------------------------------------------------------------------------
 
 // Over the four lane groups (lanes c, c + 16, c + 32, c + 48): rows are swapped between two copies of the register.

@@ -119,7 +119,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
             feed.template put<false>(sh.q, sh.d, sh.seg, masked, sh.bad[parity]);
             far = __any(feed.seg != kNoSeg && far_lse(row_lse));
             if (wave == 0) {
-                // a query whose statistics are not finite sees a non-finite value; it is marked like one that holds it
+                // a query that sees a non-finite value has NaN here, which masked pairs drop with their score
                 float less = row_lse == -INFINITY || feed.seg == kNoSeg ? 0.f : to_log2(row_lse), dl = feed.seg == kNoSeg ? 0.f : row_delta;
                 if (far) {
                     float low = 0.f;
@@ -128,10 +128,6 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
                         less = two[0], low = two[1];
                     }
                     sh.low[lane] = low;
-                }
-                if (masked && (!(fabsf(less) < INFINITY) || !(fabsf(dl) < INFINITY))) {
-                    less = dl = 0.f;
-                    atomicOr(&sh.bad[parity][lane >> 5], 1u << (lane & 31));
                 }
                 sh.less[lane] = less;
                 sh.delta[lane] = dl;
@@ -171,8 +167,10 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
             for (int n = 0; n < 4; ++n) {
                 const f32x4 dl = *reinterpret_cast<const f32x4*>(&sh.delta[16 * n + 4 * g]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dp[n][r] = s[n][r] * (dp[n][r] - dl[r]);
-                if constexpr (CAP) dp[n] *= slope[n];
+                for (int r = 0; r < 4; ++r) {
+                    dp[n][r] = weighed(s[n][r], dp[n][r] - dl[r]);
+                    if constexpr (CAP) dp[n][r] = weighed(dp[n][r], slope[n][r]);
+                }
             }
             second_product<T, DP>(dv, s, rd, sh.d);
             second_product<T, DP>(dk, dp, rd, sh.q);

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
     f32x4 dq[MEND ? 2 : 1][S::DT];                                // ds k, p k
 #pragma unroll
     for (int dt = 0; dt < S::DT; ++dt) dq[0][dt] = dq[MEND ? 1 : 0][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float seen = 0.f;                                             // sum p dp
+    float seen = less - less;                                     // sum p dp; NaN if the statistics are not finite
     // the distances that the block's pairs can have (table_near touches 76 below a pair of tiles), within kNear
     const int near_lo = q0 - (t1 - 1) * kTile - 76 > -kNear ? q0 - (t1 - 1) * kTile - 76 : -kNear;
     const int near_hi = q0 + kTile - 1 < kNear ? q0 + kTile - 1 : kNear;
@@ -179,14 +179,14 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) seen += s[n][r] * dp[n][r];
+            for (int r = 0; r < 4; ++r) seen += weighed(s[n][r], dp[n][r]);
     };
     // ds in place of the weights, and what they add to the table's gradient
     auto table_sums = [&](int t, f32x4 (&s)[4], const f32x4 (&dp)[4]) {
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[n][r] *= dp[n][r] - delta;
+            for (int r = 0; r < 4; ++r) s[n][r] = weighed(s[n][r], dp[n][r] - delta);
         if constexpr (!TABLE) return;
         const int flat = flat_of(t);
         if (flat >= 0) {
@@ -238,7 +238,9 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dq(const AttAr
 #pragma unroll
                         for (int m = 0; m <= (MEND ? 1 : 0); ++m)
 #pragma unroll
-                            for (int n = 0; n < 4; ++n) s[m][n] *= slope[n];
+                            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) s[m][n][r] = weighed(s[m][n][r], slope[n][r]);
                     }
                     second_products<T, DP>(dq, s, rd, sh.k);
                 }

@@ -176,19 +176,19 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
 #pragma unroll
             for (int n = 0; n < 4; ++n) s[n] -= far && !spoilt ? low : 0.f;
         }
-        float delta = 0.f;
+        float delta = less - less;                              // NaN if the statistics are not finite
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 s[n][r] = __builtin_amdgcn_exp2f(s[n][r]);
-                delta += s[n][r] * dp[n][r];
+                delta += weighed(s[n][r], dp[n][r]);
             }
         delta = group_sum(delta);
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) dp[n][r] = s[n][r] == 0.f ? 0.f : s[n][r] * (dp[n][r] - delta);
+            for (int r = 0; r < 4; ++r) dp[n][r] = weighed(s[n][r], dp[n][r] - delta);
         if (want_table) {
             if (flat >= 0) {
                 float sum = 0.f;
@@ -201,7 +201,9 @@ __global__ __launch_bounds__(kBlock, (Shape<T, DP>::RB > 64 ? 2 : CAP ? 3 : 4)) 
         }
         if constexpr (CAP) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) dp[n] *= slope[n];
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dp[n][r] = weighed(dp[n][r], slope[n][r]);
         }
         put_weights<T>(sh.w, s, row, g);
         put_weights<T>(sh.dz, dp, row, g);

@@ -281,3 +281,49 @@ def test_biases_far_from_zero_among_many_histories_of_one_tile(c):
     for table_gradient in (True, False):
         test_a_bias_that_all_pairs_share_changes_no_weight(c, -1e9, table_gradient)
         test_a_bias_at_the_end_of_its_type(c, "lowest", table_gradient)
+
+
+# ---- finite values whose products overflow where they are masked ------------------------------------------
+
+LOUD = [
+    case("bf16", 1, 200, 2, 1, 64, docs=True, buckets=8, far=30), case("f32", 2, 70, 2, 2, 20, docs=True, cap=5.0), case("bf16", 1, 130, 2, 2, 128),
+    case("bf16", 50, 200, 2, 2, 128, buckets=8, far=30), case("f32", 40, 130, 4, 2, 64, cap=5.0, buckets=8, far=30), case("bf16", 3, 50, 2, 2, 20, docs=True, cap=5.0, buckets=8, far=30),
+    case("f32", 1, 300, 2, 2, 128, docs=True), case("bf16", 70, 150, 4, 2, 64, docs=True, cap=5.0),
+]
+
+
+@pytest.mark.parametrize("c", LOUD, ids=name_of)
+def test_products_that_overflow_where_they_are_masked_reach_no_one(c):
+    """The first 20 positions hold a very large dout and q, the others, which those do not see, very large values and keys that cancel
+    in no order: the products of the two are infinite or no number, and have no part in the first positions' gradients."""
+    import torch
+    from paper_2204_04179_amd import gram
+    q, k, v, do, _, _, table = inputs(torch, c, seed=51)
+    B, L, n = c["B"], c["L"], 20
+    seg = torch.where(torch.arange(L) < n, 3, 4).int().expand(B, L).contiguous() if c["docs"] else None
+    do[:, :n] *= 2.0 ** 60
+    v[:, n:] *= 2.0 ** 80
+    q[:, :n] = q[:, :n].sign() * 2.0 ** 30
+    k[:, :n] *= 2.0 ** -30
+    k[:, n:] = k[:, n:].sign() * 2.0 ** 120
+    part = [t[:, :n] for t in (q, k, v, do)]
+    want = oracle_of({**c, "L": n}, *part, None, None, table)
+    got = run_gpu(torch, gram, c, q, k, v, do, seg, None, table)
+    for name in ("o", "dq"):
+        lo.assert_within(got[name][:, :n], want[name], name)
+    if c["docs"]:
+        for name in ("dk", "dv"):
+            lo.assert_within(got[name][:, :n], want[name], name)
+
+
+@pytest.mark.parametrize("c", [LOUD[0], LOUD[3], LOUD[4], LOUD[5], case("bf16", 3, 64, 2, 2, 64, causal=False)], ids=name_of)
+def test_a_query_without_a_gradient_that_sees_a_nan_has_one(c):
+    """Its dout is zero, and zero times the NaN of its weights is NaN."""
+    import torch
+    from paper_2204_04179_amd import gram
+    q, k, v, do, _, _, table = inputs(torch, c, seed=52)
+    k[:, 5], do[:] = float("nan"), 0.0
+    got = run_gpu(torch, gram, c, q, k, v, do, None, None, table)
+    assert not bool(torch.isfinite(got["dq"][:, 5:].float()).any()) and not bool(torch.isfinite(got["dv"].float()).any())
+    if c["causal"]:
+        assert bool((got["dq"][:, :5] == 0).all())
