@@ -2,7 +2,7 @@
 //
 //   dk_j = scale sum_i dz_ij q_i       dv_j = sum_i p_ij do_i       over the queries of every head that shares the key
 //
-// 1024 x 200 positions, 8 heads of 128, causal, bf16: 1.15 ms.  A block's own keys and values and its stores alone take 0.36 of
+// 1024 x 200 positions, 8 heads of 128, causal, bf16: 1.17 ms.  A block's own keys and values and its stores alone take 0.36 of
 // it, as long as the memory needs; with two waves per SIMD (the accumulators of dk and dv are 64 registers, 253 in all) little of
 // the staging and of the products hides behind the other.
 #include "gram_attend.h"
@@ -37,7 +37,7 @@ template <typename T, int DP, int UNIT, bool CAP, int WAVES, int SPLIT>
 __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttArgs a)
 {
     using S = Shape<T, DP>;
-    constexpr bool AHEAD = S::RB < 256;          // the next tile's loads under way; at 256 bytes 1.17 ms and 1.15 without
+    constexpr bool AHEAD = S::RB < 256;          // the next tile's loads under way; at 256 bytes it took 2 % longer
     __shared__ DkvShared<T, DP> sets[SPLIT];
     const int set = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kBlock) : 0;
     DkvShared<T, DP>& sh = sets[set];

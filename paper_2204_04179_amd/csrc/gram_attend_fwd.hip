@@ -6,8 +6,10 @@
 //
 // One pass over the keys with the running maximum and sum of the softmax; scores and weights stay in registers.
 //
-// 1024 x 200 positions, 8 heads of 128, causal, a table, bf16: 0.54 ms, where reading q, k, v and writing o would take 0.36 at a
-// large copy's rate.  Half of a wave's life is waiting (barriers and LDS, three waves per SIMD), a fifth vector arithmetic.
+// 1024 x 200 positions, 8 heads of 128, causal, a table, bf16: 0.53 ms, where reading q, k, v and writing o would take 0.36 at a
+// large copy's rate.  Half of a wave's life is waiting (barriers and LDS, three waves per SIMD), a fifth vector arithmetic.  float32, 8
+// heads of 64 (as many bytes): 1.05 ms, of which the products over whole tiles would take 0.57 at a large product's rate; 256 x 200,
+// 8 heads of 128: 0.54, and 0.28.
 #include "gram_attend.h"
 
 namespace gram {
@@ -29,7 +31,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend(const AttArgs 
 {
     using S = Shape<T, DP>;
     // the next tile's loads under way while this one is worked on; at 256 bytes a row the registers for it spill (1024 x 200, 8
-    // heads of 128: 0.81 ms, and 0.54 without)
+    // heads of 128: 0.81 ms, and 0.53 without)
     constexpr bool AHEAD = S::RB < 256;
     __shared__ FwdShared<T, DP> sets[SPLIT];
     const int set = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kBlock) : 0;

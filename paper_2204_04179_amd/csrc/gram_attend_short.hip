@@ -6,7 +6,7 @@
 // weights and their gradients then change hands through LDS to waves that own 16 keys.  delta comes from the tile itself.
 //
 // 128 x 55, 20 heads of 20, bf16, a table: 30 us, 34 MB at 1.1 TB/s; bound by one tile's chain of loads, products and exchanges,
-// which up to four blocks per CU overlap.  1024 x 50, 4 heads of 64: 74 us, of that the table's gradient 22.
+// which up to four blocks per CU overlap.  1024 x 50, 4 heads of 64: 70 us, of that the table's gradient 14.
 #include "gram_attend.h"
 
 namespace gram {

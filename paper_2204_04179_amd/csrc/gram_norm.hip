@@ -8,7 +8,9 @@
 // squares, so no two nearly equal numbers are subtracted.  All sums are float32; lanes are added by a butterfly, rows in
 // a fixed order, so results are the same bits run to run.  What bounds both passes is HBM: each operand is touched once.
 // 204,800 x 1024: float32 to bf16 207 us (6.1 TB/s), bf16 to bf16 156 us; backward of that with a float32 gradient added 466 us
-// (5.4 TB/s).  7,040 x 400: 5.7 and 9 us, and 4 us for the last sum.
+// (5.4 TB/s).  51,200 x 4096, bf16: 215 us (3.9 TB/s) and 502 (5.0); 25,600 x 8192: 195 and 490, in float32 339 (5.0 TB/s) and 644
+// (5.2).  7,040 x 400: 5.7 and 9.5 us, and 4.0 us for the last sum of 1.4 MB, of which a launch with nothing to add takes 2.5; 1,024
+// partial rows of 8192 columns (67 MB) take it 24.
 #include "gram_internal.h"
 
 namespace gram {
