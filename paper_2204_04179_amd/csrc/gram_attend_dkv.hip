@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
         if (AHEAD && at.t < ntiles) load(at.h, at.t);
         __syncthreads();
         const bool sees = there && wk0 < a.length && !(a.causal && q0 + kTile - 1 < wk0 && wk0 >= prefix);
-        if (sees) {
+        auto pairs = [&](auto far) {
             f32x4 s[4], dp[4], slope[CAP ? 4 : 1];
             first_product<T, DP>(s, kf, rd, sh.q);
             to_scores<CAP>(s, slope, zc, cap2, z2, a.bk.side && flat >= 0 ? to_log2(table[flat]) : 0.f);
@@ -174,6 +174,14 @@ __global__ __launch_bounds__(kBlock * SPLIT, WAVES) void k_attend_dkv(const AttA
             }
             second_product<T, DP>(dv, s, rd, sh.d);
             second_product<T, DP>(dk, dp, rd, sh.q);
+        };
+        // Rows of 512 bytes spill registers: the rare case apart keeps its own out of the usual one's way (256 x 200, 8 heads of 128, the
+        // whole backward pass 2.10 ms and 2.18).  Others only run out of instruction cache by it (1024 x 200: 2.76 and 1.80).
+        if constexpr (S::RB <= 256) {
+            if (sees) pairs(far);
+        } else if (sees) {
+            if (far) pairs(std::true_type{});
+            else pairs(std::false_type{});
         }
         parity ^= 1;
     }
