@@ -9,7 +9,7 @@
 // 1024 x 200 positions, 8 heads of 128, causal, a table, bf16: 0.53 ms, where reading q, k, v and writing o would take 0.36 at a
 // large copy's rate.  Half of a wave's life is waiting (barriers and LDS, three waves per SIMD), a fifth vector arithmetic.  float32, 8
 // heads of 64 (as many bytes): 1.05 ms, of which the products over whole tiles would take 0.57 at a large product's rate; 256 x 200,
-// 8 heads of 128: 0.54, and 0.28.
+// 8 heads of 128: 0.53, and 0.28.
 #include "gram_attend.h"
 
 namespace gram {
